@@ -260,7 +260,7 @@ def _exact_keep(seed, offset, p, n):
 
 def exact(case, seed):
     op, n, C, p = case["op"], case["rows"], case["C"], case["p"]
-    if p > 0 and n * C > 120_000_000:                  # the generator runs on the host: about 10 seconds there
+    if p > 0 and n * C > 120_000_000:                  # the generator runs on the host: seconds
         return None
     st = _inputs(case, seed)
     if p > 0:
