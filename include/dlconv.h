@@ -39,7 +39,8 @@ typedef enum {
     DL_ERR_ALIGN = 4,        /* a tensor base is not 16-byte aligned              */
     DL_ERR_WORKSPACE = 5,    /* workspace NULL or smaller than the query says     */
     DL_ERR_UNSUPPORTED = 6,  /* valid request the kernels cannot serve            */
-    DL_ERR_LAUNCH = 7        /* the HIP runtime refused a launch                  */
+    DL_ERR_LAUNCH = 7,       /* the HIP runtime refused a launch                  */
+    DL_ERR_VALUE = 8         /* a scalar argument is outside its range            */
 } dl_status;
 
 typedef enum { DL_F16 = 0, DL_BF16 = 1, DL_F32 = 2 } dl_dtype;
@@ -180,6 +181,93 @@ dl_status conv2d_transpose_bwd_filter(const dl_conv_desc *desc, const void *x, c
 dl_status dl_bias_relu_bwd_workspace_bytes(int64_t n_pixels, int32_t K, size_t *bytes);
 dl_status bias_relu_bwd(const void *dy, const void *y, int32_t dtype, int64_t n_pixels, int32_t K, int32_t relu,
                         void *dz, float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Dropout, with a mask that is drawn from a counter-based generator and never
+ * stored (paper, Sec. "Single GPU Performance": dropout is among the point-wise
+ * operations around the convolutions; each of them is a read and a write of
+ * the tensor, and a stored mask would be one more of both).  The random
+ * numbers of a call are a function of (seed, offset + *step, element index)
+ * alone, so the backward call with the same three draws the same mask, whatever
+ * ran in between:
+ *   element i takes the 16-bit field i % 8 (field 0 in the lowest bits) of the
+ *   128 bits that Philox4x32-10 makes of the counter (i / 8, offset + *step), 64
+ *   bits each, lower half first, under the key `seed`;
+ *   it is kept where that number is at least t = rint(65536 * p).
+ * So p counts in steps of 2^-16; kept elements are multiplied by
+ * 65536 / (65536 - t) (rounded to fp32), which makes the expectation exact for
+ * the p that is used.  p = 0 keeps everything, p = 1 nothing.  Calls that must not
+ * share a mask (layers, training steps) differ in offset or seed.
+ * step: DEVICE pointer to one number (8-byte aligned), read when the kernel runs,
+ * or NULL (0): a captured HIP graph holds p, seed and offset as they were, and
+ * draws other masks on its next replay where the program has changed *step. */
+typedef struct {
+    float p;                            /* 0 <= p <= 1                             */
+    uint64_t seed, offset;
+    const uint64_t *step;               /* device memory, or NULL                  */
+} dl_dropout;
+
+/* y[i] = residual[i] + (kept ? scale * x[i] : 0)  and its gradient
+ * dx[i] = kept ? scale * dy[i] : 0  (the residual's gradient is dy itself).
+ * count elements, all tensors in `dtype` (F16 | BF16 | F32), formed in fp32 and
+ * rounded once.  residual may be NULL (none).  A dropped element is chosen away:
+ * an infinity or NaN there does not reach y.  y may be x or residual, dx may be
+ * dy.  dropout: HOST pointer.  p outside 0..1: DL_ERR_VALUE.  count < 2^46. */
+dl_status dropout_fwd(const void *x, const void *residual, const dl_dropout *dropout, int32_t dtype, int64_t count,
+                      void *y, void *hip_stream);
+dl_status dropout_bwd(const void *dy, const dl_dropout *dropout, int32_t dtype, int64_t count, void *dx,
+                      void *hip_stream);
+
+/* Layer norm over the channels of each pixel (with the paper's other point-wise
+ * operations between the convolutions): x: [n_pixels, C] in `dtype` (F16 | BF16 |
+ * F32),
+ *   m = sum_c x[c] / C;  v = sum_c (x[c] - m)^2 / C;  r = 1 / sqrt(v + eps)
+ *   y[c] = (x[c] - m) * r * gamma[c] + beta[c]
+ * in fp32, rounded once.  gamma, beta: device float[C], or both NULL (1 and 0).
+ * mean, rstd: device float[n_pixels], what the backward pass takes, or NULL (not
+ * written; inference).  eps finite and >= 0 (with 0 a row of equal values has
+ * no finite r): DL_ERR_VALUE otherwise.  1 <= C <= DL_NORM_MAX_CHANNELS,
+ * n_pixels * C < 2^46.  y may be x.  float arrays need 4-byte alignment. */
+#define DL_NORM_MAX_CHANNELS 1048576
+dl_status layer_norm_fwd(const void *x, const float *gamma, const float *beta, int32_t dtype, int64_t n_pixels,
+                         int32_t C, float eps, void *y, float *mean, float *rstd, void *hip_stream);
+
+/* Gradients of layer_norm_fwd, with h = (x - m) r and g = dy * gamma:
+ *   dx = r * (g - sum_c g / C - h * sum_c (g * h) / C)
+ *   dgamma[c] = sum over pixels of dy * h;   dbeta[c] = sum over pixels of dy
+ * mean, rstd: as layer_norm_fwd left them for this x.  dgamma, dbeta: device
+ * float[C] (fp32 sums in a fixed order), or both NULL where gamma and beta are
+ * not trained (then no workspace is needed and x and dy are still read once).
+ * dx may be dy or x.  n_pixels == 0 writes dgamma = dbeta = 0.  Workspace:
+ * dl_layer_norm_bwd_workspace_bytes(n_pixels, C). */
+dl_status dl_layer_norm_bwd_workspace_bytes(int64_t n_pixels, int32_t C, size_t *bytes);
+dl_status layer_norm_bwd(const void *dy, const void *x, const float *gamma, const float *mean, const float *rstd,
+                         int32_t dtype, int64_t n_pixels, int32_t C, void *dx, float *dgamma, float *dbeta,
+                         void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* What stands between two residual blocks, in one pass over the tensors (paper,
+ * Sec. "Single GPU Performance": fusing point-wise operations so that tensors are
+ * read and written fewer times):
+ *   s = residual + dropout(x);   y = layer_norm(s)
+ * with the bits that dropout_fwd and layer_norm_fwd give one after the other (the
+ * norm is that of the rounded s; 4 tensors cross DRAM instead of 5).  residual
+ * NULL: none.  dropout NULL: nothing is dropped (inference).  s is the residual
+ * stream's next value; it may be x or residual, y may be x or residual, s and y
+ * are different tensors.  Element c of pixel n is element n * C + c of dropout_fwd.
+ * Everything else as for the two. */
+dl_status dropout_add_layer_norm_fwd(const void *x, const void *residual, const dl_dropout *dropout, const float *gamma,
+                                     const float *beta, int32_t dtype, int64_t n_pixels, int32_t C, float eps, void *s,
+                                     void *y, float *mean, float *rstd, void *hip_stream);
+
+/* Its gradients.  dy: gradient of y; ds: gradient that reaches s by the residual
+ * stream, or NULL (0); s, mean, rstd: as the forward call left them:
+ *   dresidual = ds + (dx of layer_norm_bwd at s);   dx = kept ? scale * dresidual : 0
+ * (dx from the unrounded fp32 value).  Either of dresidual and dx may be NULL (not
+ * written); without dropout they are equal.  dresidual and dx may each be dy, ds or
+ * s, and are different tensors.  dgamma, dbeta and the workspace as for layer_norm_bwd. */
+dl_status dropout_add_layer_norm_bwd(const void *dy, const void *ds, const void *s, const dl_dropout *dropout,
+                                     const float *gamma, const float *mean, const float *rstd, int32_t dtype,
+                                     int64_t n_pixels, int32_t C, void *dresidual, void *dx, float *dgamma, float *dbeta,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* LARC weight update for a list of layers (paper, Sec. "LARC": a separate learning
  * rate for every layer, the size of the update defined relative to the norm of

@@ -21,7 +21,8 @@ PASS_FWD, PASS_BWD_DATA, PASS_BWD_FILTER = 0, 1, 2
 
 EXPORTS = ("dl_conv_out_shape", "dl_conv_workspace_bytes", "dl_conv_least_workspace_bytes", "dl_conv_describe", "conv2d_fwd", "conv2d_fwd_bias_relu", "conv2d_fwd_bias_add_relu", "conv2d_bwd_data",
            "conv2d_bwd_filter", "conv2d_transpose_fwd", "conv2d_transpose_bwd_data", "conv2d_transpose_bwd_filter",
-           "dl_bias_relu_bwd_workspace_bytes", "bias_relu_bwd", "dl_larc_workspace_bytes", "larc_sgd_step", "dl_ce_workspace_bytes", "weighted_pixel_ce_fwd_bwd", "weighted_pixel_ce_fwd_bwd_static",
+           "dl_bias_relu_bwd_workspace_bytes", "bias_relu_bwd", "dropout_fwd", "dropout_bwd", "layer_norm_fwd", "dl_layer_norm_bwd_workspace_bytes", "layer_norm_bwd",
+           "dropout_add_layer_norm_fwd", "dropout_add_layer_norm_bwd", "dl_larc_workspace_bytes", "larc_sgd_step", "dl_ce_workspace_bytes", "weighted_pixel_ce_fwd_bwd", "weighted_pixel_ce_fwd_bwd_static",
            "weighted_pixel_ce_map_fwd_bwd",
            "dl_logits_ce_workspace_bytes", "logits_ce_fused_fwd_bwd", "dl_status_string")
 
@@ -71,6 +72,40 @@ class ConvDesc:
         return {k: v for k, v in self.__dict__.items() if k != "_kept"}
 
 
+class _Dropout(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+@dataclass(frozen=True, eq=False)
+class DropoutDesc:
+    """Mirror of ``dl_dropout``: which mask a call draws.  The backward call takes the forward call's.
+
+    ``seed`` and ``offset`` are 64-bit numbers; ``step`` is None or an int64 device tensor of one element that is added to the
+    offset when the kernel runs (a captured graph draws another mask on each replay if the program counts it up)."""
+    p: float
+    seed: int
+    offset: int = 0
+    step: torch.Tensor | None = None
+
+    def __post_init__(self):
+        if not 0.0 <= self.p <= 1.0:
+            raise ValueError("the probability p must lie between 0 and 1")
+        if not (0 <= self.seed < 1 << 64 and 0 <= self.offset < 1 << 64):
+            raise ValueError("seed and offset must be 64-bit numbers")
+        if self.step is not None and (self.step.dtype != torch.int64 or self.step.numel() != 1 or not self.step.is_cuda):
+            raise ValueError("step must be an int64 device tensor of one element")
+        c = _Dropout(self.p, self.seed, self.offset, None if self.step is None else self.step.data_ptr())
+        object.__setattr__(self, "_kept", ctypes.byref(c))
+
+    def __getstate__(self):
+        """The fields alone: the C structure beside them holds pointers."""
+        return {k: v for k, v in self.__dict__.items() if k != "_kept"}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self.__post_init__()
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_1810_01993_amd.build` "
@@ -88,6 +123,15 @@ def _load() -> ctypes.CDLL:
     lib.conv2d_fwd_bias_add_relu.argtypes = [dp, vp, vp, vp, vp, ctypes.c_int32, vp, vp, sz, vp]
     lib.dl_bias_relu_bwd_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(sz)]
     lib.bias_relu_bwd.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, sz, vp]
+    i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    drop = ctypes.POINTER(_Dropout)
+    lib.dropout_fwd.argtypes = [vp, vp, drop, i32, i64, vp, vp]
+    lib.dropout_bwd.argtypes = [vp, drop, i32, i64, vp, vp]
+    lib.layer_norm_fwd.argtypes = [vp, vp, vp, i32, i64, i32, f32, vp, vp, vp, vp]
+    lib.dl_layer_norm_bwd_workspace_bytes.argtypes = [i64, i32, ctypes.POINTER(sz)]
+    lib.layer_norm_bwd.argtypes = [vp, vp, vp, vp, vp, i32, i64, i32, vp, vp, vp, vp, sz, vp]
+    lib.dropout_add_layer_norm_fwd.argtypes = [vp, vp, drop, vp, vp, i32, i64, i32, f32, vp, vp, vp, vp, vp]
+    lib.dropout_add_layer_norm_bwd.argtypes = [vp, vp, vp, drop, vp, vp, vp, i32, i64, i32, vp, vp, vp, vp, vp, sz, vp]
     lib.dl_larc_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.POINTER(sz)]
     lib.larc_sgd_step.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_float, ctypes.c_float,
                                   ctypes.c_float, ctypes.c_float, ctypes.c_int32, vp, vp, sz, vp]
@@ -394,6 +438,186 @@ def bias_relu_bwd(dy: torch.Tensor, y: torch.Tensor | None, relu: bool, dz: torc
                               _dev_ptr(dz) if relu else None, _dev_ptr(dbias), _dev_ptr(ws), nb, _stream()),
            "bias_relu_bwd")
     return (dz if relu else dy), dbias
+
+
+_ROW_DTYPES = {torch.float16: DL_F16, torch.bfloat16: DL_BF16, torch.float32: DL_F32}
+
+
+def _row_tensor(t: torch.Tensor) -> int:
+    """The dtype code of a [pixels, channels] operand, which has to lie on the current device."""
+    code = _ROW_DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"fp16, bf16 or fp32 tensor required, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError("contiguous device tensor required")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError("the tensors must lie on the current device")
+    return code
+
+
+def _like(t: torch.Tensor, ref: torch.Tensor, name: str) -> int:
+    """The address of an operand that matches ref."""
+    if t.dtype != ref.dtype or t.shape != ref.shape or t.device != ref.device or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {ref.dtype} tensor of shape {tuple(ref.shape)} on {ref.device} required")
+    return t.data_ptr()
+
+
+def _vector(t: torch.Tensor, count: int, device, name: str) -> int:
+    """The address of a float32 array of count elements."""
+    if t.dtype != torch.float32 or t.numel() != count or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous float32 tensor of {count} elements on {device} required")
+    return t.data_ptr()
+
+
+def _drop(dropout: DropoutDesc | None, device):
+    """The C structure of a dropout descriptor whose step, if any, lies where the tensors do."""
+    if dropout is None:
+        return None
+    if dropout.step is not None and dropout.step.device != device:
+        raise ValueError("step must lie on the tensors' device")
+    return dropout._kept
+
+
+def dropout_fwd(x: torch.Tensor, dropout: DropoutDesc, residual: torch.Tensor | None = None,
+                y: torch.Tensor | None = None) -> torch.Tensor:
+    """y = residual + (kept ? scale * x : 0) with the mask that ``dropout`` names; x fp16, bf16 or fp32 of any shape."""
+    code = _row_tensor(x)
+    if y is None:
+        y = torch.empty_like(x)
+    _check(_lib.dropout_fwd(_like(x, x, "x"), None if residual is None else _like(residual, x, "residual"),
+                            _drop(dropout, x.device), code, x.numel(), _like(y, x, "y"), _stream()), "dropout_fwd")
+    return y
+
+
+def dropout_bwd(dy: torch.Tensor, dropout: DropoutDesc, dx: torch.Tensor | None = None) -> torch.Tensor:
+    """dx = kept ? scale * dy : 0 with the forward call's mask (the residual's gradient is dy itself)."""
+    code = _row_tensor(dy)
+    if dx is None:
+        dx = torch.empty_like(dy)
+    _check(_lib.dropout_bwd(_like(dy, dy, "dy"), _drop(dropout, dy.device), code, dy.numel(), _like(dx, dy, "dx"), _stream()),
+           "dropout_bwd")
+    return dx
+
+
+def _rows(x: torch.Tensor):
+    """(pixels, channels) of a [..., C] tensor."""
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("[..., C] tensor with C >= 1 required")
+    C = x.shape[-1]
+    return x.numel() // C, C
+
+
+def _affine(gamma, beta, C, device):
+    if gamma is None and beta is None:
+        return None, None
+    if gamma is None or beta is None:
+        raise ValueError("gamma and beta: both or neither")
+    return _vector(gamma, C, device, "gamma"), _vector(beta, C, device, "beta")
+
+
+def _stats_out(x, n, mean, rstd, want_stats):
+    if want_stats:
+        if mean is None:
+            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        if rstd is None:
+            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    m = None if mean is None else _vector(mean, n, x.device, "mean")
+    r = None if rstd is None else _vector(rstd, n, x.device, "rstd")
+    return mean, rstd, m, r
+
+
+def layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tensor | None, eps: float = 1e-5,
+                   y: torch.Tensor | None = None, mean: torch.Tensor | None = None, rstd: torch.Tensor | None = None,
+                   want_stats: bool = True):
+    """Layer norm over the last dimension: x [..., C] fp16, bf16 or fp32, gamma and beta float32[C] (or both None).  Returns
+    (y, mean, rstd); the float32 statistics [...] are for layer_norm_bwd (None with want_stats False: inference)."""
+    code = _row_tensor(x)
+    n, C = _rows(x)
+    g, b = _affine(gamma, beta, C, x.device)
+    if y is None:
+        y = torch.empty_like(x)
+    mean, rstd, m, r = _stats_out(x, n, mean, rstd, want_stats)
+    _check(_lib.layer_norm_fwd(_like(x, x, "x"), g, b, code, n, C, eps, _like(y, x, "y"), m, r, _stream()), "layer_norm_fwd")
+    return y, mean, rstd
+
+
+def dl_layer_norm_bwd_workspace_bytes(n_pixels: int, C: int) -> int:
+    need = ctypes.c_size_t(0)
+    _check(_lib.dl_layer_norm_bwd_workspace_bytes(n_pixels, C, ctypes.byref(need)), "dl_layer_norm_bwd_workspace_bytes")
+    return need.value
+
+
+def _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params):
+    """(dgamma, dbeta, their addresses, workspace and its bytes) of a backward call."""
+    if not want_params:
+        return None, None, None, None, None, 0
+    dev = dy.device
+    if dgamma is None:
+        dgamma = torch.empty(C, dtype=torch.float32, device=dev)
+    if dbeta is None:
+        dbeta = torch.empty(C, dtype=torch.float32, device=dev)
+    ws, nb = _workspace(dl_layer_norm_bwd_workspace_bytes(n, C) if workspace is None else 0, dev, workspace)
+    return dgamma, dbeta, _vector(dgamma, C, dev, "dgamma"), _vector(dbeta, C, dev, "dbeta"), ws, nb
+
+
+def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor,
+                   dx: torch.Tensor | None = None, dgamma: torch.Tensor | None = None, dbeta: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, want_params: bool = True):
+    """Gradients of layer_norm_fwd from dy, its input x and its statistics.  Returns (dx, dgamma float32[C], dbeta float32[C]);
+    with want_params False the last two are None and no workspace is needed."""
+    code = _row_tensor(dy)
+    n, C = _rows(dy)
+    dev = dy.device
+    if dx is None:
+        dx = torch.empty_like(dy)
+    dgamma, dbeta, dg, db, ws, nb = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
+    _check(_lib.layer_norm_bwd(_like(dy, dy, "dy"), _like(x, dy, "x"), None if gamma is None else _vector(gamma, C, dev, "gamma"),
+                               _vector(mean, n, dev, "mean"), _vector(rstd, n, dev, "rstd"), code, n, C, _like(dx, dy, "dx"),
+                               dg, db, _dev_ptr(ws), nb, _stream()), "layer_norm_bwd")
+    return dx, dgamma, dbeta
+
+
+def dropout_add_layer_norm_fwd(x: torch.Tensor, residual: torch.Tensor | None, dropout: DropoutDesc | None,
+                               gamma: torch.Tensor | None, beta: torch.Tensor | None, eps: float = 1e-5,
+                               s: torch.Tensor | None = None, y: torch.Tensor | None = None, mean: torch.Tensor | None = None,
+                               rstd: torch.Tensor | None = None, want_stats: bool = True):
+    """s = residual + dropout(x), y = layer_norm(s) in one pass, with the bits of the two calls.  residual None: none; dropout
+    None: nothing is dropped.  Returns (s, y, mean, rstd)."""
+    code = _row_tensor(x)
+    n, C = _rows(x)
+    g, b = _affine(gamma, beta, C, x.device)
+    if s is None:
+        s = torch.empty_like(x)
+    if y is None:
+        y = torch.empty_like(x)
+    mean, rstd, m, r = _stats_out(x, n, mean, rstd, want_stats)
+    _check(_lib.dropout_add_layer_norm_fwd(_like(x, x, "x"), None if residual is None else _like(residual, x, "residual"),
+                                           _drop(dropout, x.device), g, b, code, n, C, eps, _like(s, x, "s"), _like(y, x, "y"),
+                                           m, r, _stream()), "dropout_add_layer_norm_fwd")
+    return s, y, mean, rstd
+
+
+def dropout_add_layer_norm_bwd(dy: torch.Tensor, ds: torch.Tensor | None, s: torch.Tensor, dropout: DropoutDesc | None,
+                               gamma: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor,
+                               dresidual: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+                               dgamma: torch.Tensor | None = None, dbeta: torch.Tensor | None = None,
+                               workspace: torch.Tensor | None = None, want_params: bool = True):
+    """Gradients of dropout_add_layer_norm_fwd: dy reaches y, ds (or None) reaches s by the residual stream.  Returns
+    (dresidual, dx, dgamma, dbeta); the last two are None with want_params False."""
+    code = _row_tensor(dy)
+    n, C = _rows(dy)
+    dev = dy.device
+    if dresidual is None:
+        dresidual = torch.empty_like(dy)
+    if dx is None:
+        dx = torch.empty_like(dy)
+    dgamma, dbeta, dg, db, ws, nb = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
+    _check(_lib.dropout_add_layer_norm_bwd(_like(dy, dy, "dy"), None if ds is None else _like(ds, dy, "ds"), _like(s, dy, "s"),
+                                           _drop(dropout, dev), None if gamma is None else _vector(gamma, C, dev, "gamma"),
+                                           _vector(mean, n, dev, "mean"), _vector(rstd, n, dev, "rstd"), code, n, C,
+                                           _like(dresidual, dy, "dresidual"), _like(dx, dy, "dx"), dg, db, _dev_ptr(ws), nb,
+                                           _stream()), "dropout_add_layer_norm_bwd")
+    return dresidual, dx, dgamma, dbeta
 
 
 class _LarcTensor(ctypes.Structure):

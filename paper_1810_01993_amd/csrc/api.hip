@@ -437,6 +437,7 @@ const char *dl_status_string(dl_status s)
         case DL_ERR_WORKSPACE: return "workspace missing or too small";
         case DL_ERR_UNSUPPORTED: return "unsupported configuration";
         case DL_ERR_LAUNCH: return "HIP launch failed";
+        case DL_ERR_VALUE: return "scalar argument outside its range";
     }
     return "unknown status";
 }
@@ -838,6 +839,153 @@ dl_status bias_relu_bwd(const void *dy, const void *y, int32_t dtype, int64_t n_
     a.K = K;
     a.relu = relu ? 1 : 0;
     return hip_status(dlk::launch_tail_bwd(a, dtype == DL_BF16, static_cast<hipStream_t>(hip_stream)));
+}
+
+namespace {
+constexpr int64_t MAX_ROW_ELEMS = int64_t(1) << 46;      // the [pixels][channels] kernels count in 64 bits
+
+inline bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline bool row_dtype(int32_t dtype) { return dtype == DL_F16 || dtype == DL_BF16 || dtype == DL_F32; }
+inline bool row_shape(int64_t n, int32_t C)
+{
+    return n >= 0 && C >= 1 && C <= DL_NORM_MAX_CHANNELS && n < MAX_ROW_ELEMS / C;
+}
+
+// The generator's arguments; none (nothing dropped) for a null pointer.
+dl_status drop_args(const dl_dropout *d, dlk::DropArgs *a)
+{
+    *a = dlk::DropArgs{0, 1.f, 0, 0, 0, nullptr};
+    if (!d) return DL_OK;
+    if (!(d->p >= 0.f && d->p <= 1.f)) return DL_ERR_VALUE;
+    if (!aligned_to(d->step, 8)) return DL_ERR_ALIGN;
+    a->t = (uint32_t)std::lrint((double)d->p * 65536.0);
+    a->scale = a->t < 65536u ? 65536.f / (float)(65536u - a->t) : 0.f;
+    a->k0 = (uint32_t)d->seed;
+    a->k1 = (uint32_t)(d->seed >> 32);
+    a->offset = d->offset;
+    a->step = d->step;
+    return DL_OK;
+}
+
+dl_status run_dropout(const void *x, const void *residual, const dl_dropout *d, int32_t dtype, int64_t count, void *y,
+                      void *hip_stream)
+{
+    if (!d || (count > 0 && (!x || !y))) return DL_ERR_NULL;
+    if (count < 0 || count >= MAX_ROW_ELEMS) return DL_ERR_SHAPE;
+    if (!row_dtype(dtype)) return DL_ERR_DTYPE;
+    dlk::DropoutArgs a{};
+    const dl_status st = drop_args(d, &a.drop);
+    if (st != DL_OK) return st;
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(y)) return DL_ERR_ALIGN;
+    a.x = x;
+    a.residual = residual;
+    a.y = y;
+    a.n = count;
+    return hip_status(dlk::launch_dropout(a, dtype, static_cast<hipStream_t>(hip_stream)));
+}
+
+dl_status run_norm_fwd(dlk::LayerNormArgs a, const dl_dropout *d, int32_t dtype, void *hip_stream)
+{
+    if (a.n > 0 && (!a.x || !a.y || (a.joined && !a.s))) return DL_ERR_NULL;
+    if (!a.gamma != !a.beta) return DL_ERR_NULL;
+    if (!row_shape(a.n, a.C)) return DL_ERR_SHAPE;
+    if (!row_dtype(dtype)) return DL_ERR_DTYPE;
+    if (!(a.eps >= 0.f) || std::isinf(a.eps)) return DL_ERR_VALUE;
+    const dl_status st = drop_args(d, &a.drop);
+    if (st != DL_OK) return st;
+    if (!aligned16(a.x) || !aligned16(a.residual) || !aligned16(a.s) || !aligned16(a.y) || !aligned_to(a.gamma, 4) ||
+        !aligned_to(a.beta, 4) || !aligned_to(a.mean, 4) || !aligned_to(a.rstd, 4))
+        return DL_ERR_ALIGN;
+    return hip_status(dlk::launch_layer_norm_fwd(a, dtype, static_cast<hipStream_t>(hip_stream)));
+}
+
+dl_status run_norm_bwd(dlk::LayerNormArgs a, const dl_dropout *d, int32_t dtype, void *workspace, size_t workspace_bytes,
+                       void *hip_stream)
+{
+    if (!a.dgamma != !a.dbeta) return DL_ERR_NULL;
+    if (a.n > 0 && (!a.dy || !a.x || !a.mean || !a.rstd || !(a.dx || (a.joined && a.dres)))) return DL_ERR_NULL;
+    if (!row_shape(a.n, a.C)) return DL_ERR_SHAPE;
+    if (!row_dtype(dtype)) return DL_ERR_DTYPE;
+    const dl_status st = drop_args(d, &a.drop);
+    if (st != DL_OK) return st;
+    if (!aligned16(a.dy) || !aligned16(a.x) || !aligned16(a.ds) || !aligned16(a.dres) || !aligned16(a.dx) || !aligned_to(a.gamma, 4) ||
+        !aligned_to(a.mean, 4) || !aligned_to(a.rstd, 4) || !aligned_to(a.dgamma, 4) || !aligned_to(a.dbeta, 4))
+        return DL_ERR_ALIGN;
+    if (a.dgamma) {
+        a.slabs = dlk::layer_norm_slabs(a.n, a.C);
+        if (!workspace || workspace_bytes < (size_t)a.slabs * 2 * a.C * sizeof(float)) return DL_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return DL_ERR_ALIGN;
+        a.partial = static_cast<float *>(workspace);
+    }
+    return hip_status(dlk::launch_layer_norm_bwd(a, dtype, static_cast<hipStream_t>(hip_stream)));
+}
+}  // namespace
+
+dl_status dropout_fwd(const void *x, const void *residual, const dl_dropout *dropout, int32_t dtype, int64_t count,
+                      void *y, void *hip_stream)
+{
+    return run_dropout(x, residual, dropout, dtype, count, y, hip_stream);
+}
+
+dl_status dropout_bwd(const void *dy, const dl_dropout *dropout, int32_t dtype, int64_t count, void *dx, void *hip_stream)
+{
+    return run_dropout(dy, nullptr, dropout, dtype, count, dx, hip_stream);
+}
+
+dl_status layer_norm_fwd(const void *x, const float *gamma, const float *beta, int32_t dtype, int64_t n_pixels, int32_t C,
+                         float eps, void *y, float *mean, float *rstd, void *hip_stream)
+{
+    dlk::LayerNormArgs a{};
+    a.x = x; a.y = y;
+    a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
+    a.n = n_pixels; a.C = C; a.eps = eps;
+    return run_norm_fwd(a, nullptr, dtype, hip_stream);
+}
+
+dl_status dropout_add_layer_norm_fwd(const void *x, const void *residual, const dl_dropout *dropout, const float *gamma,
+                                     const float *beta, int32_t dtype, int64_t n_pixels, int32_t C, float eps, void *s,
+                                     void *y, float *mean, float *rstd, void *hip_stream)
+{
+    if (s && s == y) return DL_ERR_UNSUPPORTED;
+    dlk::LayerNormArgs a{};
+    a.x = x; a.residual = residual; a.s = s; a.y = y;
+    a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
+    a.n = n_pixels; a.C = C; a.eps = eps; a.joined = 1;
+    return run_norm_fwd(a, dropout, dtype, hip_stream);
+}
+
+dl_status dl_layer_norm_bwd_workspace_bytes(int64_t n_pixels, int32_t C, size_t *bytes)
+{
+    if (!bytes) return DL_ERR_NULL;
+    if (!row_shape(n_pixels, C)) return DL_ERR_SHAPE;
+    *bytes = (size_t)dlk::layer_norm_slabs(n_pixels, C) * 2 * C * sizeof(float);
+    return DL_OK;
+}
+
+dl_status layer_norm_bwd(const void *dy, const void *x, const float *gamma, const float *mean, const float *rstd,
+                         int32_t dtype, int64_t n_pixels, int32_t C, void *dx, float *dgamma, float *dbeta, void *workspace,
+                         size_t workspace_bytes, void *hip_stream)
+{
+    dlk::LayerNormArgs a{};
+    a.dy = dy; a.x = x; a.dx = dx;
+    a.gamma = gamma; a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
+    a.dgamma = dgamma; a.dbeta = dbeta;
+    a.n = n_pixels; a.C = C;
+    return run_norm_bwd(a, nullptr, dtype, workspace, workspace_bytes, hip_stream);
+}
+
+dl_status dropout_add_layer_norm_bwd(const void *dy, const void *ds, const void *s, const dl_dropout *dropout,
+                                     const float *gamma, const float *mean, const float *rstd, int32_t dtype,
+                                     int64_t n_pixels, int32_t C, void *dresidual, void *dx, float *dgamma, float *dbeta,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (dx && dx == dresidual) return DL_ERR_UNSUPPORTED;
+    dlk::LayerNormArgs a{};
+    a.dy = dy; a.ds = ds; a.x = s; a.dres = dresidual; a.dx = dx;
+    a.gamma = gamma; a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
+    a.dgamma = dgamma; a.dbeta = dbeta;
+    a.n = n_pixels; a.C = C; a.joined = 1;
+    return run_norm_bwd(a, dropout, dtype, workspace, workspace_bytes, hip_stream);
 }
 
 dl_status dl_larc_workspace_bytes(int32_t n_tensors, size_t *bytes)

@@ -349,6 +349,43 @@ struct LarcBatch {
 };
 hipError_t launch_larc(const LarcBatch &b, int grad_dtype, hipStream_t stream);
 
+// Dropout's generator and threshold (see rows.h): an element is kept where its 16-bit number is at least t.
+struct DropArgs {
+    uint32_t t;                 // 0 (nothing is dropped) .. 65536 (everything is)
+    float scale;                // of the kept elements
+    uint32_t k0, k1;            // key
+    uint64_t offset;            // upper half of the counter,
+    const uint64_t *step;       // to which the number at this device address is added, if any
+};
+// y = residual + dropout(x) on n elements; residual may be null.
+struct DropoutArgs {
+    const void *x, *residual;
+    void *y;
+    int64_t n;
+    DropArgs drop;
+};
+hipError_t launch_dropout(const DropoutArgs &a, int dtype, hipStream_t stream);
+
+// Layer norm over [n][C] and its backward pass (see layer_norm.hip).
+struct LayerNormArgs {
+    const void *x;              // forward: the input (of the dropout, if joined); backward: what was normalised
+    const void *residual;       // joined forward, or null
+    void *s, *y;                // s: joined forward
+    const void *dy, *ds;        // ds: joined backward, or null
+    void *dres, *dx;            // either may be null in the joined backward
+    const float *gamma, *beta;  // both or none
+    float *mean, *rstd;         // written by the forward pass where not null, read by the backward pass
+    float *dgamma, *dbeta;      // both or none
+    float *partial;             // [slabs][2][C]
+    int64_t n, chunk;           // chunk: pixels per slab (set by the launcher)
+    int32_t C, slabs, joined;
+    float eps;
+    DropArgs drop;
+};
+int layer_norm_slabs(int64_t n, int C);
+hipError_t launch_layer_norm_fwd(const LayerNormArgs &a, int dtype, hipStream_t stream);
+hipError_t launch_layer_norm_bwd(const LayerNormArgs &a, int dtype, hipStream_t stream);
+
 // Weighted per-pixel cross-entropy, 3 classes.
 int ce_num_blocks(int64_t n_pixels);
 // The logits layer (1x1, C -> 3) fused with the loss: one pass over x.  C % 8 == 0, 32 <= C <= 2048.
