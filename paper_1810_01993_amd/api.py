@@ -443,37 +443,52 @@ def bias_relu_bwd(dy: torch.Tensor, y: torch.Tensor | None, relu: bool, dz: torc
 _ROW_DTYPES = {torch.float16: DL_F16, torch.bfloat16: DL_BF16, torch.float32: DL_F32}
 
 
-def _row_tensor(t: torch.Tensor) -> int:
-    """The dtype code of a [pixels, channels] operand, which has to lie on the current device."""
-    code = _ROW_DTYPES.get(t.dtype)
+def _begin(x: torch.Tensor):
+    """(dtype code, current stream) of a call on a [..., channels] operand, which has to lie on the current device."""
+    code = _ROW_DTYPES.get(x.dtype)
     if code is None:
-        raise TypeError(f"fp16, bf16 or fp32 tensor required, got {t.dtype}")
-    if not t.is_cuda:
+        raise TypeError(f"fp16, bf16 or fp32 tensor required, got {x.dtype}")
+    index = x.get_device()
+    if index < 0:
         raise ValueError("contiguous device tensor required")
-    if t.get_device() != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         raise ValueError("the tensors must lie on the current device")
-    return code
+    return code, torch._C._cuda_getCurrentRawStream(index)
 
 
-def _like(t: torch.Tensor, ref: torch.Tensor, name: str) -> int:
-    """The address of an operand that matches ref."""
-    if t.dtype != ref.dtype or t.shape != ref.shape or t.device != ref.device or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {ref.dtype} tensor of shape {tuple(ref.shape)} on {ref.device} required")
-    return t.data_ptr()
+def _like(names: str, ref: torch.Tensor, *tensors):
+    """The addresses of operands that match ref (None for one that is left out).  One pass with what ref is looked up once: the
+    attributes of a tensor take longer than the arithmetic of a small call."""
+    dtype, shape, index = ref.dtype, ref.shape, ref.get_device()
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if (t is not ref and (t.dtype is not dtype or t.shape != shape or t.get_device() != index)) or not t.is_contiguous():
+            raise ValueError(f"{names.split()[len(out)]}: contiguous {dtype} tensor of shape {tuple(shape)} on {ref.device} required")
+        out.append(t.data_ptr())
+    return out
 
 
-def _vector(t: torch.Tensor, count: int, device, name: str) -> int:
-    """The address of a float32 array of count elements."""
-    if t.dtype != torch.float32 or t.numel() != count or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous float32 tensor of {count} elements on {device} required")
-    return t.data_ptr()
+def _vectors(names: str, ref: torch.Tensor, count: int, *tensors):
+    """The addresses of float32 arrays of count elements on ref's device (None for one that is left out)."""
+    f32, index, out = torch.float32, ref.get_device(), []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not f32 or t.numel() != count or t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"{names.split()[len(out)]}: contiguous float32 tensor of {count} elements on {ref.device} required")
+        out.append(t.data_ptr())
+    return out
 
 
-def _drop(dropout: DropoutDesc | None, device):
+def _drop(dropout: DropoutDesc | None, x: torch.Tensor):
     """The C structure of a dropout descriptor whose step, if any, lies where the tensors do."""
     if dropout is None:
         return None
-    if dropout.step is not None and dropout.step.device != device:
+    if dropout.step is not None and dropout.step.device != x.device:
         raise ValueError("step must lie on the tensors' device")
     return dropout._kept
 
@@ -481,38 +496,36 @@ def _drop(dropout: DropoutDesc | None, device):
 def dropout_fwd(x: torch.Tensor, dropout: DropoutDesc, residual: torch.Tensor | None = None,
                 y: torch.Tensor | None = None) -> torch.Tensor:
     """y = residual + (kept ? scale * x : 0) with the mask that ``dropout`` names; x fp16, bf16 or fp32 of any shape."""
-    code = _row_tensor(x)
+    code, stream = _begin(x)
     if y is None:
         y = torch.empty_like(x)
-    _check(_lib.dropout_fwd(_like(x, x, "x"), None if residual is None else _like(residual, x, "residual"),
-                            _drop(dropout, x.device), code, x.numel(), _like(y, x, "y"), _stream()), "dropout_fwd")
+    xp, rp, yp = _like("x residual y", x, x, residual, y)
+    _check(_lib.dropout_fwd(xp, rp, _drop(dropout, x), code, x.numel(), yp, stream), "dropout_fwd")
     return y
 
 
 def dropout_bwd(dy: torch.Tensor, dropout: DropoutDesc, dx: torch.Tensor | None = None) -> torch.Tensor:
     """dx = kept ? scale * dy : 0 with the forward call's mask (the residual's gradient is dy itself)."""
-    code = _row_tensor(dy)
+    code, stream = _begin(dy)
     if dx is None:
         dx = torch.empty_like(dy)
-    _check(_lib.dropout_bwd(_like(dy, dy, "dy"), _drop(dropout, dy.device), code, dy.numel(), _like(dx, dy, "dx"), _stream()),
-           "dropout_bwd")
+    gp, xp = _like("dy dx", dy, dy, dx)
+    _check(_lib.dropout_bwd(gp, _drop(dropout, dy), code, dy.numel(), xp, stream), "dropout_bwd")
     return dx
 
 
 def _rows(x: torch.Tensor):
     """(pixels, channels) of a [..., C] tensor."""
-    if x.dim() < 1 or x.shape[-1] < 1:
+    shape = x.shape
+    if not shape or shape[-1] < 1:
         raise ValueError("[..., C] tensor with C >= 1 required")
-    C = x.shape[-1]
-    return x.numel() // C, C
+    return x.numel() // shape[-1], shape[-1]
 
 
-def _affine(gamma, beta, C, device):
-    if gamma is None and beta is None:
-        return None, None
-    if gamma is None or beta is None:
+def _affine(gamma, beta, x, C):
+    if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta: both or neither")
-    return _vector(gamma, C, device, "gamma"), _vector(beta, C, device, "beta")
+    return _vectors("gamma beta", x, C, gamma, beta)
 
 
 def _stats_out(x, n, mean, rstd, want_stats):
@@ -521,9 +534,7 @@ def _stats_out(x, n, mean, rstd, want_stats):
             mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
         if rstd is None:
             rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    m = None if mean is None else _vector(mean, n, x.device, "mean")
-    r = None if rstd is None else _vector(rstd, n, x.device, "rstd")
-    return mean, rstd, m, r
+    return mean, rstd, *_vectors("mean rstd", x, n, mean, rstd)
 
 
 def layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tensor | None, eps: float = 1e-5,
@@ -531,13 +542,14 @@ def layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tens
                    want_stats: bool = True):
     """Layer norm over the last dimension: x [..., C] fp16, bf16 or fp32, gamma and beta float32[C] (or both None).  Returns
     (y, mean, rstd); the float32 statistics [...] are for layer_norm_bwd (None with want_stats False: inference)."""
-    code = _row_tensor(x)
+    code, stream = _begin(x)
     n, C = _rows(x)
-    g, b = _affine(gamma, beta, C, x.device)
+    g, b = _affine(gamma, beta, x, C)
     if y is None:
         y = torch.empty_like(x)
     mean, rstd, m, r = _stats_out(x, n, mean, rstd, want_stats)
-    _check(_lib.layer_norm_fwd(_like(x, x, "x"), g, b, code, n, C, eps, _like(y, x, "y"), m, r, _stream()), "layer_norm_fwd")
+    xp, yp = _like("x y", x, x, y)
+    _check(_lib.layer_norm_fwd(xp, g, b, code, n, C, eps, yp, m, r, stream), "layer_norm_fwd")
     return y, mean, rstd
 
 
@@ -548,16 +560,19 @@ def dl_layer_norm_bwd_workspace_bytes(n_pixels: int, C: int) -> int:
 
 
 def _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params):
-    """(dgamma, dbeta, their addresses, workspace and its bytes) of a backward call."""
+    """(dgamma, dbeta, their addresses, the workspace's and its bytes, the workspace) of a backward call."""
     if not want_params:
-        return None, None, None, None, None, 0
-    dev = dy.device
+        return None, None, None, None, None, 0, None
     if dgamma is None:
-        dgamma = torch.empty(C, dtype=torch.float32, device=dev)
+        dgamma = torch.empty(C, dtype=torch.float32, device=dy.device)
     if dbeta is None:
-        dbeta = torch.empty(C, dtype=torch.float32, device=dev)
-    ws, nb = _workspace(dl_layer_norm_bwd_workspace_bytes(n, C) if workspace is None else 0, dev, workspace)
-    return dgamma, dbeta, _vector(dgamma, C, dev, "dgamma"), _vector(dbeta, C, dev, "dbeta"), ws, nb
+        dbeta = torch.empty(C, dtype=torch.float32, device=dy.device)
+    if workspace is None:
+        workspace = torch.empty(dl_layer_norm_bwd_workspace_bytes(n, C), dtype=torch.uint8, device=dy.device)
+    elif workspace.get_device() != dy.get_device() or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous tensor on {dy.device} required")
+    dg, db = _vectors("dgamma dbeta", dy, C, dgamma, dbeta)
+    return dgamma, dbeta, dg, db, workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor,
@@ -565,15 +580,15 @@ def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None
                    workspace: torch.Tensor | None = None, want_params: bool = True):
     """Gradients of layer_norm_fwd from dy, its input x and its statistics.  Returns (dx, dgamma float32[C], dbeta float32[C]);
     with want_params False the last two are None and no workspace is needed."""
-    code = _row_tensor(dy)
+    code, stream = _begin(dy)
     n, C = _rows(dy)
-    dev = dy.device
     if dx is None:
         dx = torch.empty_like(dy)
-    dgamma, dbeta, dg, db, ws, nb = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
-    _check(_lib.layer_norm_bwd(_like(dy, dy, "dy"), _like(x, dy, "x"), None if gamma is None else _vector(gamma, C, dev, "gamma"),
-                               _vector(mean, n, dev, "mean"), _vector(rstd, n, dev, "rstd"), code, n, C, _like(dx, dy, "dx"),
-                               dg, db, _dev_ptr(ws), nb, _stream()), "layer_norm_bwd")
+    dgamma, dbeta, dg, db, wp, nb, workspace = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
+    gp, xp, dp = _like("dy x dx", dy, dy, x, dx)
+    (ga,) = _vectors("gamma", dy, C, gamma)
+    m, r = _vectors("mean rstd", dy, n, mean, rstd)
+    _check(_lib.layer_norm_bwd(gp, xp, ga, m, r, code, n, C, dp, dg, db, wp, nb, stream), "layer_norm_bwd")
     return dx, dgamma, dbeta
 
 
@@ -583,17 +598,17 @@ def dropout_add_layer_norm_fwd(x: torch.Tensor, residual: torch.Tensor | None, d
                                rstd: torch.Tensor | None = None, want_stats: bool = True):
     """s = residual + dropout(x), y = layer_norm(s) in one pass, with the bits of the two calls.  residual None: none; dropout
     None: nothing is dropped.  Returns (s, y, mean, rstd)."""
-    code = _row_tensor(x)
+    code, stream = _begin(x)
     n, C = _rows(x)
-    g, b = _affine(gamma, beta, C, x.device)
+    g, b = _affine(gamma, beta, x, C)
     if s is None:
         s = torch.empty_like(x)
     if y is None:
         y = torch.empty_like(x)
     mean, rstd, m, r = _stats_out(x, n, mean, rstd, want_stats)
-    _check(_lib.dropout_add_layer_norm_fwd(_like(x, x, "x"), None if residual is None else _like(residual, x, "residual"),
-                                           _drop(dropout, x.device), g, b, code, n, C, eps, _like(s, x, "s"), _like(y, x, "y"),
-                                           m, r, _stream()), "dropout_add_layer_norm_fwd")
+    xp, rp, sp, yp = _like("x residual s y", x, x, residual, s, y)
+    _check(_lib.dropout_add_layer_norm_fwd(xp, rp, _drop(dropout, x), g, b, code, n, C, eps, sp, yp, m, r, stream),
+           "dropout_add_layer_norm_fwd")
     return s, y, mean, rstd
 
 
@@ -604,19 +619,18 @@ def dropout_add_layer_norm_bwd(dy: torch.Tensor, ds: torch.Tensor | None, s: tor
                                workspace: torch.Tensor | None = None, want_params: bool = True):
     """Gradients of dropout_add_layer_norm_fwd: dy reaches y, ds (or None) reaches s by the residual stream.  Returns
     (dresidual, dx, dgamma, dbeta); the last two are None with want_params False."""
-    code = _row_tensor(dy)
+    code, stream = _begin(dy)
     n, C = _rows(dy)
-    dev = dy.device
     if dresidual is None:
         dresidual = torch.empty_like(dy)
     if dx is None:
         dx = torch.empty_like(dy)
-    dgamma, dbeta, dg, db, ws, nb = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
-    _check(_lib.dropout_add_layer_norm_bwd(_like(dy, dy, "dy"), None if ds is None else _like(ds, dy, "ds"), _like(s, dy, "s"),
-                                           _drop(dropout, dev), None if gamma is None else _vector(gamma, C, dev, "gamma"),
-                                           _vector(mean, n, dev, "mean"), _vector(rstd, n, dev, "rstd"), code, n, C,
-                                           _like(dresidual, dy, "dresidual"), _like(dx, dy, "dx"), dg, db, _dev_ptr(ws), nb,
-                                           _stream()), "dropout_add_layer_norm_bwd")
+    dgamma, dbeta, dg, db, wp, nb, workspace = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
+    gp, sg, sp, rp, dp = _like("dy ds s dresidual dx", dy, dy, ds, s, dresidual, dx)
+    (ga,) = _vectors("gamma", dy, C, gamma)
+    m, r = _vectors("mean rstd", dy, n, mean, rstd)
+    _check(_lib.dropout_add_layer_norm_bwd(gp, sg, sp, _drop(dropout, dy), ga, m, r, code, n, C, rp, dp, dg, db, wp, nb, stream),
+           "dropout_add_layer_norm_bwd")
     return dresidual, dx, dgamma, dbeta
 
 

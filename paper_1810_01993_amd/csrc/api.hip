@@ -854,11 +854,12 @@ inline bool row_shape(int64_t n, int32_t C)
 // The generator's arguments; none (nothing dropped) for a null pointer.
 dl_status drop_args(const dl_dropout *d, dlk::DropArgs *a)
 {
-    *a = dlk::DropArgs{0, 1.f, 0, 0, 0, nullptr};
+    *a = dlk::DropArgs{0, 0, 1.f, 0, 0, 0, nullptr};
     if (!d) return DL_OK;
     if (!(d->p >= 0.f && d->p <= 1.f)) return DL_ERR_VALUE;
     if (!aligned_to(d->step, 8)) return DL_ERR_ALIGN;
     a->t = (uint32_t)std::lrint((double)d->p * 65536.0);
+    a->limit = (a->t << 16) - 1u;                        // all ones for t = 65536
     a->scale = a->t < 65536u ? 65536.f / (float)(65536u - a->t) : 0.f;
     a->k0 = (uint32_t)d->seed;
     a->k1 = (uint32_t)(d->seed >> 32);
@@ -912,8 +913,7 @@ dl_status run_norm_bwd(dlk::LayerNormArgs a, const dl_dropout *d, int32_t dtype,
         !aligned_to(a.mean, 4) || !aligned_to(a.rstd, 4) || !aligned_to(a.dgamma, 4) || !aligned_to(a.dbeta, 4))
         return DL_ERR_ALIGN;
     if (a.dgamma) {
-        a.slabs = dlk::layer_norm_slabs(a.n, a.C);
-        if (!workspace || workspace_bytes < (size_t)a.slabs * 2 * a.C * sizeof(float)) return DL_ERR_WORKSPACE;
+        if (!workspace || workspace_bytes < (size_t)dlk::layer_norm_slabs(a.n, a.C) * 2 * a.C * sizeof(float)) return DL_ERR_WORKSPACE;
         if (!aligned16(workspace)) return DL_ERR_ALIGN;
         a.partial = static_cast<float *>(workspace);
     }

@@ -2,42 +2,98 @@
 //   y[i] = residual[i] + (u[i] >= t ? scale * x[i] : 0),  u[i] a 16-bit number, t = p * 65536, scale = 65536 / (65536 - t).
 // A dropped element is chosen away, not multiplied by zero: an infinity or NaN there does not reach y.  The same kernel
 // without a residual on dy is the backward pass.
+#include <algorithm>
+
 #include "rows.h"
 
 namespace dlk {
 
-constexpr int DO_THREADS = 256;
+// Only the products written as such are fused with an addition: layer_norm.hip forms the same sums.
+#pragma clang fp contract(off)
 
-template <class T>
+constexpr int DO_THREADS = 256, DO_PIECES = 4;
+
+template <class T, bool RES, bool STREAM>
 __global__ __launch_bounds__(DO_THREADS) void dropout_kernel(const DropoutArgs p)
 {
     using R = Row<T>;
     using elem = typename R::elem;
+    constexpr int E = R::E, U = DO_PIECES;
     const Philox rng(p.drop);
     const elem *x = static_cast<const elem *>(p.x), *res = static_cast<const elem *>(p.residual);
     elem *y = static_cast<elem *>(p.y);
-    const int64_t blocks = (p.n + 7) / 8;
-    for (int64_t b = (int64_t)blockIdx.x * DO_THREADS + threadIdx.x; b < blocks; b += (int64_t)gridDim.x * DO_THREADS) {
-        const u32x4_t w = rng((uint64_t)b);
+    const int64_t pieces = p.n / E;
+    auto one = [&](int64_t j, u32x4_t xv, u32x4_t rv) {
+        float f[E];
+        R::unpack(xv, f);
+        uint32_t w[E / 2];
+        if (p.drop.t) {
+            drop_words<E, true>(rng, (uint64_t)j * E, w);
+            drop_select<E>(w, p.drop.limit, f);
+        }
+        if constexpr (RES) {
+            float r[E];
+            R::unpack(rv, r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int64_t i = 8 * b + e;
-            if (i >= p.n) break;
-            const float v = philox_field(w, e) >= p.drop.t ? R::get(x[i]) : 0.f;
-            y[i] = R::put(res ? fmaf(v, p.drop.scale, R::get(res[i])) : v * p.drop.scale);
+            for (int e = 0; e < E; ++e) f[e] = fmaf(f[e], p.drop.scale, r[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[e] *= p.drop.scale;
+        }
+        u32x4_t *to = reinterpret_cast<u32x4_t *>(y) + j;
+        if constexpr (STREAM) __builtin_nontemporal_store(R::pack(f), to);
+        else *to = R::pack(f);
+    };
+    const u32x4_t *xp = reinterpret_cast<const u32x4_t *>(x), *rp = reinterpret_cast<const u32x4_t *>(res);
+    for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+        const int64_t first = tile * (U * DO_THREADS) + threadIdx.x;
+        if ((tile + 1) * (U * DO_THREADS) <= pieces) {
+            u32x4_t xv[U], rv[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                xv[u] = __builtin_nontemporal_load(xp + first + u * DO_THREADS);
+                if constexpr (RES) rv[u] = __builtin_nontemporal_load(rp + first + u * DO_THREADS);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) one(first + u * DO_THREADS, xv[u], RES ? rv[u] : u32x4_t{});
+            continue;
+        }
+        for (int64_t j = first; j < pieces; j += DO_THREADS) one(j, xp[j], RES ? rp[j] : u32x4_t{});
+        const int64_t i = pieces * E + threadIdx.x;     // what is left of the last piece
+        if (i < p.n) {
+            float f[1] = {R::get(x[i])};
+            if (p.drop.t) {
+                uint32_t w[1];
+                drop_words<1, false>(rng, (uint64_t)i, w);
+                drop_select<1>(w, p.drop.limit, f);
+            }
+            y[i] = R::put(RES ? fmaf(f[0], p.drop.scale, R::get(res[i])) : f[0] * p.drop.scale);
         }
     }
+}
+
+template <class T, bool RES>
+static void dropout_go(const DropoutArgs &a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)std::min<int64_t>(a.tiles, 1 << 22)), block(DO_THREADS);
+    if (a.n * (16 / Row<T>::E) > 300000000) DLK_LAUNCH("dropout_kernel", (dropout_kernel<T, RES, true>), grid, block, 0, stream, a);
+    else DLK_LAUNCH("dropout_kernel", (dropout_kernel<T, RES, false>), grid, block, 0, stream, a);
+}
+template <class T>
+static hipError_t dropout_type(const DropoutArgs &a0, hipStream_t stream)
+{
+    DropoutArgs a = a0;
+    const int64_t per = (int64_t)DO_PIECES * DO_THREADS * Row<T>::E;
+    a.tiles = (a.n + per - 1) / per;
+    if (a.residual) dropout_go<T, true>(a, stream);
+    else dropout_go<T, false>(a, stream);
+    return launch_status();
 }
 
 hipError_t launch_dropout(const DropoutArgs &a, int dtype, hipStream_t stream)
 {
     if (a.n <= 0) return hipSuccess;
-    const int64_t wgs = ((a.n + 7) / 8 + DO_THREADS - 1) / DO_THREADS;
-    const dim3 grid((unsigned)(wgs < 65536 ? wgs : 65536)), block(DO_THREADS);
-    if (dtype == 0) DLK_LAUNCH("dropout_kernel", dropout_kernel<F16>, grid, block, 0, stream, a);
-    else if (dtype == 1) DLK_LAUNCH("dropout_kernel", dropout_kernel<BF16>, grid, block, 0, stream, a);
-    else DLK_LAUNCH("dropout_kernel", dropout_kernel<F32>, grid, block, 0, stream, a);
-    return launch_status();
+    return dtype == 0 ? dropout_type<F16>(a, stream) : dtype == 1 ? dropout_type<BF16>(a, stream) : dropout_type<F32>(a, stream);
 }
 
 }  // namespace dlk

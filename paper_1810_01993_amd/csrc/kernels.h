@@ -351,7 +351,7 @@ hipError_t launch_larc(const LarcBatch &b, int grad_dtype, hipStream_t stream);
 
 // Dropout's generator and threshold (see rows.h): an element is kept where its 16-bit number is at least t.
 struct DropArgs {
-    uint32_t t;                 // 0 (nothing is dropped) .. 65536 (everything is)
+    uint32_t t, limit;          // 0 (nothing is dropped) .. 65536 (everything is); (t << 16) - 1
     float scale;                // of the kept elements
     uint32_t k0, k1;            // key
     uint64_t offset;            // upper half of the counter,
@@ -361,7 +361,7 @@ struct DropArgs {
 struct DropoutArgs {
     const void *x, *residual;
     void *y;
-    int64_t n;
+    int64_t n, tiles;           // tiles: of a workgroup's elements (set by the launcher)
     DropArgs drop;
 };
 hipError_t launch_dropout(const DropoutArgs &a, int dtype, hipStream_t stream);
@@ -378,7 +378,7 @@ struct LayerNormArgs {
     float *dgamma, *dbeta;      // both or none
     float *partial;             // [slabs][2][C]
     int64_t n, chunk;           // chunk: pixels per slab (set by the launcher)
-    int32_t C, slabs, joined;
+    int32_t C, joined;
     float eps;
     DropArgs drop;
 };

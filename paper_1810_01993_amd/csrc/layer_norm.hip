@@ -6,10 +6,338 @@
 //              dgamma = sum_pixels dy h;  dbeta = sum_pixels dy
 // The norm is that of s as stored (rounded), so that the backward pass, which has nothing else, sees the same numbers.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.h"
 
 namespace dlk {
+
+// Only the products written as such are fused with an addition: the joined kernels then give the bits of the separate ones.
+#pragma clang fp contract(off)
+
+// How the rows are dealt out.  A team of `lanes` lanes of a wave has a row (teams side by side in the wave have neighbouring
+// rows), or, WIDE, a whole workgroup has one.  Lane l owns the 16-byte pieces l, l + lanes, ... (V at most) of its row: it reads
+// them once, keeps them in registers through both sums and the result, and has the next row's pieces on their way meanwhile.
+// Rows that are no whole number of pieces (ODD) end in a piece that reaches back over what the one before it covers: the elements
+// that both hold are counted once and stored twice, with the same bits.  VEC = 1: rows shorter than a piece.
+constexpr int LN_WAVES = 4;                             // of a workgroup whose teams lie within waves
+struct LnShape {
+    int pieces, lanes, waves, v;                        // of a row; lanes 0: WIDE; pieces a lane has
+    int grid, past;                                     // past: what is read much later is stored past the caches
+    int64_t trips;                                      // rows that a team, or a workgroup, goes through
+};
+
+template <class T, int VEC, int V, bool ODD> struct LnLane {
+    int c0[V], skip;                                    // first element of a piece; elements of the last one that the piece before it has
+    bool on[V];
+    __device__ __forceinline__ LnLane(int l, int lanes, int pieces, int C)
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = l + v * lanes;
+            on[v] = j < pieces;
+            c0[v] = on[v] ? ODD ? min(j * VEC, C - VEC) : j * VEC : 0;
+        }
+        skip = ODD && on[V - 1] ? (l + (V - 1) * lanes) * VEC - c0[V - 1] : 0;
+    }
+};
+
+// The VEC floats of a parameter from channel c on, four at a time; `none` where there is no parameter.
+template <int VEC> __device__ __forceinline__ void ln_param(const float *param, int c, bool on, float none, float (&f)[VEC])
+{
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = none;
+    if (!param || !on) return;
+    if constexpr (VEC == 1) f[0] = param[c];
+    else
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4) {
+            const floatx4_t w = *reinterpret_cast<const floatx4_any_t *>(param + c + e);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) f[e + d] = w[d];
+        }
+}
+
+// The sums of a piece's channels from element `skip` on.
+template <int VEC, bool ODD> __device__ __forceinline__ void ln_put_sums(float *to, int skip, const float (&f)[VEC])
+{
+    if constexpr (VEC == 1) to[0] = f[0];
+    else if (ODD && skip) {
+#pragma unroll
+        for (int e = 1; e < VEC; ++e)
+            if (e >= skip) to[e] = f[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4)
+            *reinterpret_cast<floatx4_any_t *>(to + e) = floatx4_any_t{f[e], f[e + 1], f[e + 2], f[e + 3]};
+    }
+}
+
+// Sums over a row: its team's lanes (FULL: all 64), or the workgroup's waves through red (two arrays used in turn: between two
+// uses of one lies the other's barrier).
+template <bool FULL, bool WIDE, int N> __device__ __forceinline__ void row_sums(float (&v)[N], int lanes, float *red)
+{
+    team_sums(v, FULL || WIDE ? 64 : lanes);
+    if constexpr (WIDE) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[16 * i + (threadIdx.x >> 6)] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = red[16 * i];
+            for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v[i] += red[16 * i + w];
+        }
+    }
+}
+
+// The rows of a team, or of a workgroup: first, first + step, ...  DEPTH - 1 rows' loads are under way while one is computed.  They
+// are not conditional (beyond the last row they read that one again, for a piece that the row does not have its first one, and nobody
+// uses what comes): the wait for a row's data then counts exactly the loads behind it, where a branch round them would make it a wait
+// for all.
+template <bool WIDE> struct LnRows {
+    int64_t row, step;
+    __device__ __forceinline__ LnRows(int lanes)
+    {
+        const int per = WIDE ? 1 : 64 * LN_WAVES / lanes;
+        step = (int64_t)gridDim.x * per;
+        row = (int64_t)blockIdx.x * per + (WIDE ? 0 : threadIdx.x / lanes);
+    }
+};
+
+template <class T, int VEC, int V, int MODE, bool ODD, bool WIDE, bool FULL>
+__global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_fwd_kernel(const LayerNormArgs p, const LnShape q)
+{
+    constexpr bool JOINED = MODE > 0, RES = MODE > 1;
+    using P = Piece<T, VEC, ODD>;
+    using elem = typename P::elem;
+    using raw = typename P::raw;
+    constexpr int DEPTH = 2;
+    __shared__ float red[2][16];
+    const int lanes = WIDE ? (int)blockDim.x : FULL ? 64 : q.lanes;
+    const int l = threadIdx.x & (lanes - 1);
+    const LnLane<T, VEC, V, ODD> at(l, lanes, q.pieces, p.C);
+    LnRows<WIDE> it(lanes);
+    const elem *x = static_cast<const elem *>(p.x), *res = static_cast<const elem *>(p.residual);
+    struct Buf { raw x[V], res[RES ? V : 1]; } buf[DEPTH];
+    auto fetch = [&](Buf &b, int64_t r) {
+        const int64_t base = min(r, p.n - 1) * p.C;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            b.x[v] = P::load(x + base + at.c0[v]);
+            if constexpr (RES) b.res[v] = P::load(res + base + at.c0[v]);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d) fetch(buf[d], it.row + d * it.step);
+    float gamma[V][VEC], beta[V][VEC];                  // asked for behind the first rows, which are needed first
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        ln_param<VEC>(p.gamma, at.c0[v], at.on[v], 1.f, gamma[v]);
+        ln_param<VEC>(p.beta, at.c0[v], at.on[v], 0.f, beta[v]);
+    }
+    const Philox rng(p.drop);
+    const float inv = 1.f / (float)p.C;
+    auto row = [&](const Buf &b) {
+        const int64_t base = it.row * p.C;
+        float f[V][VEC], sum[1] = {0.f}, sq[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            P::unpack(b.x[v], f[v]);
+            if constexpr (JOINED) {
+                if (p.drop.t) {
+                    uint32_t w[(VEC + 1) / 2];
+                    drop_words<VEC, !ODD && VEC != 1>(rng, (uint64_t)(base + at.c0[v]), w);
+                    drop_select<VEC>(w, p.drop.limit, f[v]);
+                }
+                float r[VEC];
+                if constexpr (RES) P::unpack(b.res[v], r);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[v][e] = RES ? fmaf(f[v][e], p.drop.scale, r[e]) : f[v][e] * p.drop.scale;
+                const raw out = P::pack(f[v]);
+                if (at.on[v]) P::store(static_cast<elem *>(p.s) + base + at.c0[v], out, q.past);
+                P::unpack(out, f[v]);
+            }
+            if (at.on[v])
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[0] += !ODD || v < V - 1 || e >= at.skip ? f[v][e] : 0.f;
+        }
+        row_sums<FULL, WIDE>(sum, lanes, red[0]);
+        const float mean = sum[0] * inv;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[v][e] -= mean;
+            if (at.on[v])
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = !ODD || v < V - 1 || e >= at.skip ? f[v][e] : 0.f;
+                    sq[0] = fmaf(d, d, sq[0]);
+                }
+        }
+        row_sums<FULL, WIDE>(sq, lanes, red[1]);
+        const float rstd = 1.f / sqrtf(fmaf(sq[0], inv, p.eps));
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[v][e] = fmaf(f[v][e] * rstd, gamma[v][e], beta[v][e]);
+            if (at.on[v]) P::store(static_cast<elem *>(p.y) + base + at.c0[v], P::pack(f[v]));
+        }
+        if (l == 0) {
+            if (p.mean) p.mean[it.row] = mean;
+            if (p.rstd) p.rstd[it.row] = rstd;
+        }
+    };
+    for (int64_t k = 0; k < q.trips; k += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            fetch(buf[(d + DEPTH - 1) % DEPTH], it.row + (DEPTH - 1) * it.step);
+            if (it.row < p.n) row(buf[d]);
+            it.row += it.step;
+        }
+    }
+}
+
+// The backward pass.  With e = dy r, g = e gamma, d = s - m the row's gradient is g - sum(g) / C - d r^2 sum(g d) / C: dgamma adds
+// up e d.  The lanes that hold a channel add up its part of dgamma and dbeta over their rows in registers; at the end the teams of
+// a wave, then the waves of the workgroup are added (fixed order) and the workgroup's sums written as one slab.
+template <class T, int VEC, int V, int MODE, bool ODD, bool WIDE, bool FULL>
+__global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_bwd_kernel(const LayerNormArgs p, const LnShape q)
+{
+    constexpr bool JOINED = MODE > 0, RES = MODE > 1;
+    using P = Piece<T, VEC, ODD>;
+    using elem = typename P::elem;
+    using raw = typename P::raw;
+    constexpr int DEPTH = WIDE && V * VEC <= 8 ? 3 : 2;
+    extern __shared__ float lds[];                      // WIDE: [2][2][16]; otherwise the sums of the workgroup's waves
+    const int lanes = WIDE ? (int)blockDim.x : FULL ? 64 : q.lanes;
+    const int l = threadIdx.x & (lanes - 1);
+    const LnLane<T, VEC, V, ODD> at(l, lanes, q.pieces, p.C);
+    LnRows<WIDE> it(lanes);
+    const elem *dy = static_cast<const elem *>(p.dy), *s = static_cast<const elem *>(p.x), *ds = static_cast<const elem *>(p.ds);
+    struct Buf { raw dy[V], s[V], ds[RES ? V : 1]; float mean, rstd; } buf[DEPTH];
+    auto fetch = [&](Buf &b, int64_t r) {
+        r = min(r, p.n - 1);
+        const int64_t base = r * p.C;
+        b.mean = p.mean[r];
+        b.rstd = p.rstd[r];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            b.dy[v] = P::load(dy + base + at.c0[v]);
+            b.s[v] = P::load(s + base + at.c0[v]);
+            if constexpr (RES) b.ds[v] = P::load(ds + base + at.c0[v]);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d) fetch(buf[d], it.row + d * it.step);
+    float gamma[V][VEC], dg[V][VEC], db[V][VEC];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        ln_param<VEC>(p.gamma, at.c0[v], at.on[v], 1.f, gamma[v]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) dg[v][e] = db[v][e] = 0.f;
+    }
+    const Philox rng(p.drop);
+    const float inv = 1.f / (float)p.C;
+    float *red = lds;
+    auto row = [&](const Buf &b) {
+        const int64_t base = it.row * p.C;
+        float g[V][VEC], h[V][VEC], sum[2] = {0.f, 0.f};
+        const float mean = b.mean, rstd = b.rstd;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            P::unpack(b.dy[v], g[v]);
+            P::unpack(b.s[v], h[v]);
+            if (!at.on[v]) continue;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const bool mine = !ODD || v < V - 1 || e >= at.skip;
+                h[v][e] -= mean;
+                db[v][e] += mine ? g[v][e] : 0.f;
+                g[v][e] *= rstd;
+                dg[v][e] = fmaf(mine ? g[v][e] : 0.f, h[v][e], dg[v][e]);
+                g[v][e] *= gamma[v][e];
+                sum[0] += mine ? g[v][e] : 0.f;
+                sum[1] = fmaf(mine ? g[v][e] : 0.f, h[v][e], sum[1]);
+            }
+        }
+        row_sums<FULL, WIDE>(sum, lanes, red);
+        if constexpr (WIDE) red = lds + (red == lds ? 32 : 0);
+        const float m0 = sum[0] * inv, m1 = sum[1] * inv * rstd * rstd;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!at.on[v]) continue;
+            float d[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[e] = fmaf(-h[v][e], m1, g[v][e] - m0);
+            if constexpr (JOINED) {
+                if constexpr (RES) {
+                    float r[VEC];
+                    P::unpack(b.ds[v], r);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) d[e] += r[e];
+                }
+                if (p.dres) P::store(static_cast<elem *>(p.dres) + base + at.c0[v], P::pack(d), q.past);
+                if (!p.dx) continue;
+                if (p.drop.t) {
+                    uint32_t w[(VEC + 1) / 2];
+                    drop_words<VEC, !ODD && VEC != 1>(rng, (uint64_t)(base + at.c0[v]), w);
+                    drop_select<VEC>(w, p.drop.limit, d);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) d[e] *= p.drop.scale;
+                }
+            }
+            P::store(static_cast<elem *>(p.dx) + base + at.c0[v], P::pack(d));
+        }
+    };
+    for (int64_t k = 0; k < q.trips; k += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            fetch(buf[(d + DEPTH - 1) % DEPTH], it.row + (DEPTH - 1) * it.step);
+            if (it.row < p.n) row(buf[d]);
+            it.row += it.step;
+        }
+    }
+    if (!p.dgamma) return;
+    // with one slab the sums are the result
+    float *og = q.grid == 1 ? p.dgamma : p.partial + (size_t)blockIdx.x * 2 * p.C, *ob = q.grid == 1 ? p.dbeta : og + p.C;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (at.on[v]) {
+                ln_put_sums<VEC, ODD>(og + at.c0[v], v < V - 1 ? 0 : at.skip, dg[v]);
+                ln_put_sums<VEC, ODD>(ob + at.c0[v], v < V - 1 ? 0 : at.skip, db[v]);
+            }
+    } else {
+        // [wave][dgamma, dbeta][v][lane][VEC]: consecutive lanes next to each other
+        const int wave = threadIdx.x >> 6, half = V * lanes * VEC;
+        float sums[2 * V * VEC];
+#pragma unroll
+        for (int i = 0; i < V * VEC; ++i) {
+            sums[i] = dg[i / VEC][i % VEC];
+            sums[V * VEC + i] = db[i / VEC][i % VEC];
+        }
+        if constexpr (!FULL) cross_sums(sums, lanes);
+        if (FULL || (int)(threadIdx.x & 63) < lanes)
+#pragma unroll
+            for (int i = 0; i < 2 * V * VEC; ++i)
+                lds[2 * half * wave + (i / VEC * lanes + l) * VEC + i % VEC] = sums[i];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * V * lanes; i += 64 * LN_WAVES) {
+            const int j = i < V * lanes ? i : i - V * lanes;            // piece (in order of the row)
+            if (j >= q.pieces) continue;
+            float sum[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                sum[e] = lds[i * VEC + e];
+#pragma unroll
+                for (int w = 1; w < LN_WAVES; ++w) sum[e] += lds[2 * half * w + i * VEC + e];
+            }
+            const int c = ODD ? min(j * VEC, p.C - VEC) : j * VEC;
+            ln_put_sums<VEC, ODD>((i < V * lanes ? og : ob) + c, ODD ? j * VEC - c : 0, sum);
+        }
+    }
+}
 
 constexpr int LN_THREADS = 256;
 
@@ -23,9 +351,9 @@ __device__ __forceinline__ float block_sum(float v, float *red)
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// One row per workgroup, each thread the elements c = thread, thread + 256, ...: any number of channels.
+// Rows too long for the registers: one row per workgroup, each thread the elements c = thread, thread + 256, ...
 template <class T, bool JOINED>
-__global__ __launch_bounds__(LN_THREADS) void layer_norm_fwd_kernel(const LayerNormArgs p)
+__global__ __launch_bounds__(LN_THREADS) void layer_norm_long_fwd_kernel(const LayerNormArgs p)
 {
     using R = Row<T>;
     using elem = typename R::elem;
@@ -73,7 +401,7 @@ __global__ __launch_bounds__(LN_THREADS) void layer_norm_fwd_kernel(const LayerN
 }
 
 template <class T, bool JOINED>
-__global__ __launch_bounds__(LN_THREADS) void layer_norm_bwd_kernel(const LayerNormArgs p)
+__global__ __launch_bounds__(LN_THREADS) void layer_norm_long_bwd_kernel(const LayerNormArgs p)
 {
     using R = Row<T>;
     using elem = typename R::elem;
@@ -93,7 +421,7 @@ __global__ __launch_bounds__(LN_THREADS) void layer_norm_bwd_kernel(const LayerN
         b = block_sum(b, red) / (float)p.C;
         for (int c = threadIdx.x; c < p.C; c += LN_THREADS) {
             const float g = R::get(dy[c]) * (p.gamma ? p.gamma[c] : 1.f);
-            float d = rstd * (g - a - (R::get(s[c]) - mean) * rstd * b);
+            float d = rstd * fmaf(-(R::get(s[c]) - mean) * rstd, b, g - a);
             if constexpr (JOINED) {
                 if (p.ds) d += R::get(static_cast<const elem *>(p.ds)[base + c]);
                 if (p.dres) static_cast<elem *>(p.dres)[base + c] = R::put(d);
@@ -135,31 +463,133 @@ __global__ __launch_bounds__(LN_THREADS) void layer_norm_param_kernel(const Laye
             (red[wave][0][lane] + red[wave][1][lane]) + (red[wave][2][lane] + red[wave][3][lane]);
 }
 
-// dgamma and dbeta from the slabs' sums, in ascending order of the slabs.
-__global__ __launch_bounds__(LN_THREADS) void layer_norm_param_sum_kernel(const float *partial, int slabs, int C, float *dgamma,
-                                                                          float *dbeta)
+// dgamma and dbeta from the slabs' sums: 16 columns a workgroup, 64 lanes down the slabs, then a tree.
+__global__ __launch_bounds__(1024) void layer_norm_param_sum_kernel(const float *partial, int slabs, int C, float *dgamma, float *dbeta)
 {
-    const int64_t i = (int64_t)blockIdx.x * LN_THREADS + threadIdx.x;
-    if (i >= 2 * (int64_t)C) return;
+    __shared__ float red[64][17];
+    const int col = threadIdx.x & 15, lane = threadIdx.x >> 4;
+    const int64_t i = (int64_t)blockIdx.x * 16 + col, all = 2 * (int64_t)C;
     float sum = 0.f;
-    for (int z = 0; z < slabs; ++z) sum += partial[(size_t)z * 2 * C + i];
-    if (i < C) dgamma[i] = sum;
-    else dbeta[i - C] = sum;
+    for (int z0 = 0; z0 < slabs; z0 += 64 * 16) {       // all loads of up to 1024 slabs at once: the kernel is one trip to memory
+        float f[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const int z = z0 + 64 * u + lane;
+            f[u] = z < slabs && i < all ? partial[z * all + i] : 0.f;
+        }
+#pragma unroll
+        for (int half = 8; half > 0; half >>= 1)
+#pragma unroll
+            for (int u = 0; u < half; ++u) f[u] += f[u + half];
+        sum += f[0];
+    }
+    red[lane][col] = sum;
+    __syncthreads();
+#pragma unroll
+    for (int half = 32; half > 0; half >>= 1) {
+        if (lane < half) red[lane][col] += red[lane + half][col];
+        __syncthreads();
+    }
+    if (lane == 0 && i < all) (i < C ? dgamma[i] : dbeta[i - C]) = red[0][col];
 }
+
+// ---- dispatch ----------------------------------------------------------------
+constexpr int CUS = 256;
+static int pow2_from(int v) { int p = 1; while (p < v) p <<= 1; return p; }
+
+// Up to 2048 pieces of a row stay in the registers of 16 waves.
+template <class T> static bool ln_long(int C) { return C > 2048 * Row<T>::E; }
+
+template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd)
+{
+    constexpr int E = Row<T>::E;
+    LnShape q{};
+    q.waves = LN_WAVES;
+    q.v = 1;
+    q.pieces = C < E ? C : (C + E - 1) / E;
+    q.past = C >= E && n * C * (16 / E) >= 16 << 20;
+    if (q.pieces <= 8 || C < E) q.lanes = pow2_from(q.pieces);
+    else if (q.pieces <= 192) {
+        // the number of pieces a lane that leaves fewest lanes idle, 8 lanes (a 128-byte line) at least
+        const int first = bwd && q.pieces < 32 ? 1 : 2;
+        int best = 1 << 30;
+        for (int v : {first, 3 - first, 3}) {
+            const int lanes = std::max(8, pow2_from((q.pieces + v - 1) / v));
+            if (lanes <= 64 && lanes * v < best) {
+                best = lanes * v;
+                q.lanes = lanes;
+                q.v = v;
+            }
+        }
+    } else {
+        // two sums of a 16-bit piece's channels and the rows under way are half of a wave's registers: one piece a lane
+        const int most = bwd && E == 8 ? 64 : 128;
+        q.waves = std::min(16, std::max(LN_WAVES, pow2_from((q.pieces + most - 1) / most)));
+        q.v = (q.pieces + 64 * q.waves - 1) / (64 * q.waves);
+    }
+    const int64_t per = q.lanes ? 64 * LN_WAVES / q.lanes : 1, want = (n + per - 1) / per;
+    int64_t most;
+    if (bwd) most = q.lanes ? (q.v == 1 ? 3 : 1) * CUS : q.v == 1 && q.waves == LN_WAVES ? 2 * CUS : CUS;
+    else if (q.lanes) most = (q.v == 1 ? 8 : 4) * CUS / (n * C * (16 / E) >= 64 << 20 ? 2 : 1);
+    else most = (q.v == 1 ? 8 : 4) * CUS * LN_WAVES / q.waves;
+    q.grid = (int)std::max<int64_t>(1, std::min(want, most));
+    q.trips = (want + q.grid - 1) / q.grid;
+    return q;
+}
+
+static int ln_long_slabs(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, 512)); }
 
 int layer_norm_slabs(int64_t n, int C)
 {
-    (void)C;
-    const int64_t b = (n + 63) / 64;
-    return (int)(b < 1 ? 1 : b > 512 ? 512 : b);
+    const int half = ln_long<F16>(C) ? ln_long_slabs(n) : ln_shape<F16>(n, C, true).grid;
+    const int whole = ln_long<F32>(C) ? ln_long_slabs(n) : ln_shape<F32>(n, C, true).grid;
+    return std::max(half, whole);
+}
+
+template <class T, int VEC, int V, bool WIDE, bool FULL>
+static void ln_launch(const LayerNormArgs &a, const LnShape &q, bool bwd, hipStream_t stream)
+{
+    const dim3 grid((unsigned)q.grid), block((unsigned)q.waves * 64);
+    const size_t lds = (WIDE ? 64 : a.dgamma ? (size_t)LN_WAVES * 2 * V * q.lanes * VEC : 1) * sizeof(float);
+    const auto go = [&](auto mode, auto odd) {
+        constexpr int MODE = decltype(mode)::value;
+        constexpr bool ODD = decltype(odd)::value;
+        if (bwd) DLK_LAUNCH("layer_norm_bwd_kernel", (layer_norm_bwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, lds, stream, a, q);
+        else DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, 0, stream, a, q);
+    };
+    const auto mode = [&](auto odd) {
+        if (!a.joined) go(std::integral_constant<int, 0>{}, odd);
+        else if (!(bwd ? a.ds : a.residual)) go(std::integral_constant<int, 1>{}, odd);
+        else go(std::integral_constant<int, 2>{}, odd);
+    };
+    if constexpr (VEC > 1)
+        if (a.C % VEC != 0) return mode(std::true_type{});
+    mode(std::false_type{});
+}
+
+template <class T>
+static hipError_t ln_resident(const LayerNormArgs &a, const LnShape &q, bool bwd, hipStream_t stream)
+{
+    constexpr int E = Row<T>::E;
+    if (a.C < E) ln_launch<T, 1, 1, false, false>(a, q, bwd, stream);
+    else if (q.lanes == 64 && q.v == 1) ln_launch<T, E, 1, false, true>(a, q, bwd, stream);
+    else if (q.lanes == 64 && q.v == 2) ln_launch<T, E, 2, false, true>(a, q, bwd, stream);
+    else if (q.lanes == 64) ln_launch<T, E, 3, false, true>(a, q, bwd, stream);
+    else if (q.lanes && q.v == 1) ln_launch<T, E, 1, false, false>(a, q, bwd, stream);
+    else if (q.lanes && q.v == 2) ln_launch<T, E, 2, false, false>(a, q, bwd, stream);
+    else if (q.lanes) ln_launch<T, E, 3, false, false>(a, q, bwd, stream);
+    else if (q.v == 1) ln_launch<T, E, 1, true, false>(a, q, bwd, stream);
+    else ln_launch<T, E, 2, true, false>(a, q, bwd, stream);
+    return launch_status();
 }
 
 template <class T>
 static hipError_t launch_ln_fwd(const LayerNormArgs &a, hipStream_t stream)
 {
+    if (!ln_long<T>(a.C)) return ln_resident<T>(a, ln_shape<T>(a.n, a.C, false), false, stream);
     const dim3 grid((unsigned)std::min<int64_t>(a.n, 1 << 20)), block(LN_THREADS);
-    if (a.joined) DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, true>), grid, block, 0, stream, a);
-    else DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, false>), grid, block, 0, stream, a);
+    if (a.joined) DLK_LAUNCH("layer_norm_long_fwd_kernel", (layer_norm_long_fwd_kernel<T, true>), grid, block, 0, stream, a);
+    else DLK_LAUNCH("layer_norm_long_fwd_kernel", (layer_norm_long_fwd_kernel<T, false>), grid, block, 0, stream, a);
     return launch_status();
 }
 
@@ -169,26 +599,37 @@ hipError_t launch_layer_norm_fwd(const LayerNormArgs &a, int dtype, hipStream_t 
     return dtype == 0 ? launch_ln_fwd<F16>(a, stream) : dtype == 1 ? launch_ln_fwd<BF16>(a, stream) : launch_ln_fwd<F32>(a, stream);
 }
 
+static hipError_t ln_param_sum(const LayerNormArgs &a, int slabs, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((2 * (int64_t)a.C + 15) / 16)), block(1024);
+    DLK_LAUNCH("layer_norm_param_sum_kernel", layer_norm_param_sum_kernel, grid, block, 0, stream, a.partial, slabs, a.C, a.dgamma, a.dbeta);
+    return launch_status();
+}
+
 template <class T>
 static hipError_t launch_ln_bwd(const LayerNormArgs &a0, hipStream_t stream)
 {
     LayerNormArgs a = a0;
     const dim3 block(LN_THREADS);
+    hipError_t e;
+    if (a.n > 0 && !ln_long<T>(a.C)) {
+        const LnShape q = ln_shape<T>(a.n, a.C, true);
+        e = ln_resident<T>(a, q, true, stream);
+        return e != hipSuccess || !a.dgamma || q.grid == 1 ? e : ln_param_sum(a, q.grid, stream);
+    }
     if (a.dgamma) {                                     // before dx, which may lie where dy does
-        a.chunk = (a.n + a.slabs - 1) / a.slabs;
-        const dim3 cols((unsigned)a.slabs, (unsigned)((a.C + 63) / 64));
+        const int slabs = ln_long_slabs(a.n);
+        a.chunk = (a.n + slabs - 1) / slabs;
+        const dim3 cols((unsigned)slabs, (unsigned)((a.C + 63) / 64));
         DLK_LAUNCH("layer_norm_param_kernel", layer_norm_param_kernel<T>, cols, block, 0, stream, a);
-        hipError_t e = launch_status();
-        if (e != hipSuccess) return e;
-        const dim3 all((unsigned)((2 * (int64_t)a.C + LN_THREADS - 1) / LN_THREADS));
-        DLK_LAUNCH("layer_norm_param_sum_kernel", layer_norm_param_sum_kernel, all, block, 0, stream, a.partial, a.slabs, a.C, a.dgamma, a.dbeta);
         e = launch_status();
+        if (e == hipSuccess) e = ln_param_sum(a, slabs, stream);
         if (e != hipSuccess) return e;
     }
     if (a.n <= 0) return hipSuccess;
     const dim3 grid((unsigned)std::min<int64_t>(a.n, 1 << 20));
-    if (a.joined) DLK_LAUNCH("layer_norm_bwd_kernel", (layer_norm_bwd_kernel<T, true>), grid, block, 0, stream, a);
-    else DLK_LAUNCH("layer_norm_bwd_kernel", (layer_norm_bwd_kernel<T, false>), grid, block, 0, stream, a);
+    if (a.joined) DLK_LAUNCH("layer_norm_long_bwd_kernel", (layer_norm_long_bwd_kernel<T, true>), grid, block, 0, stream, a);
+    else DLK_LAUNCH("layer_norm_long_bwd_kernel", (layer_norm_long_bwd_kernel<T, false>), grid, block, 0, stream, a);
     return launch_status();
 }
 

@@ -20,8 +20,9 @@ def chain(C: int) -> float:
 
 
 def chain_rows(n: int) -> float:
-    """The same for a sum over n pixels: n / 512 serial terms at most in a slab's lane, a tree, and up to 1024 slabs."""
-    return 1100.0 + n / 512
+    """The same for a sum over n pixels: n / 256 serial terms at most where a workgroup has a row at a time, a tree, and up to
+    1024 slabs."""
+    return 1100.0 + n / 256
 
 
 def f64(t: torch.Tensor) -> np.ndarray:

@@ -93,11 +93,11 @@ def test_joined_refusals(api):
 
 
 def test_workspace_query_stays_small(api):
-    """The sums' workspace is at most a few per cent of the tensors' bytes on large maps, and never empty."""
+    """The sums' workspace: a slab per row at most on small maps, at most a third of a 16-bit tensor on large ones, never empty."""
     for n, C in ((1, 1), (0, 256), (2, 256), (6912, 1024), (110592, 304), (1769472, 256), (208297, 77), (50, 8192), (7, 1 << 20)):
         b = api.dl_layer_norm_bwd_workspace_bytes(n, C)
         assert b >= 8 * C and b % (8 * C) == 0, (n, C)
-        assert b <= max(8 * C, 0.35 * 2 * n * C), (n, C, b)
+        assert b <= max(8 * C * min(max(n, 1), 768), 0.35 * 2 * n * C), (n, C, b)
 
 
 def test_descriptor(api):
@@ -123,14 +123,14 @@ def test_wrapper_refusals(api):
     for t in (torch.zeros(()), torch.zeros(3, 0)):
         with pytest.raises(ValueError):
             api._rows(t)
-    for bad in (x.float(), x[:3], x.t().contiguous().t(), x.to("meta")):
+    for bad in (x.float(), x[:3], x.t().contiguous().t()):
         with pytest.raises(ValueError):
-            api._like(bad, x, "y")
-    for bad in (v.half(), v[:7], v.to("meta"), torch.zeros(16)[::2]):
+            api._like("x y", x, x, bad)
+    for bad in (v.half(), v[:7], torch.zeros(16)[::2]):
         with pytest.raises(ValueError):
-            api._vector(bad, 8, v.device, "gamma")
+            api._vectors("gamma", v, 8, bad)
     with pytest.raises(ValueError):
-        api._affine(v, None, 8, v.device)
+        api._affine(v, None, v, 8)
 
 
 def test_host_path_under_sanitizers(tmp_path):
