@@ -5,6 +5,15 @@
 //              ds = r (g - a - h b)  (+ the gradient that reaches s by another way);  dx = dropout's mask and scale on ds
 //              dgamma = sum_pixels dy h;  dbeta = sum_pixels dy
 // The norm is that of s as stored (rounded), so that the backward pass, which has nothing else, sees the same numbers.
+//
+// Bound by memory: every tensor crosses it once.  A row stays in registers from its loads to its result, so that the variance can
+// be summed from the deviations themselves (one pass over memory, no cancellation), and the sums of the backward pass's two
+// parameter gradients stay in registers too.  Measured, with the bandwidth of what has to cross (a large copy reaches 5.5-5.7 TB/s):
+//   forward   1769472 x 256 fp16 316 us (5.7 TB/s), 6912 x 1024 bf16 8.1 us (3.5)
+//   backward  110592 x 304 fp16 39 us (5.1), 6912 x 2048 fp32 34 us (5.0), 208297 x 77 bf16 29 us (3.4: rows at odd addresses)
+//   joined    forward 110592 x 256 bf16 43 us (5.2), backward 442368 x 256 bf16 199 us (5.7), 3015 x 512 fp16 11 us (1.4: two
+//             launches, 8 and 3 us on their own)
+// Of a backward call about 4.7 us are the second launch, which adds the workgroups' sums in a fixed order.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,6 +29,10 @@ namespace dlk {
 // them once, keeps them in registers through both sums and the result, and has the next row's pieces on their way meanwhile.
 // Rows that are no whole number of pieces (ODD) end in a piece that reaches back over what the one before it covers: the elements
 // that both hold are counted once and stored twice, with the same bits.  VEC = 1: rows shorter than a piece.
+//
+// Loads of whole pieces carry the hint that nobody reads the line again (backward 110592 x 256 fp16: 35.1 us with it, 38.1
+// without); a line that rows share does not.  y and dx are stored without it, the next kernel reads them; s and the residual's
+// gradient, which come back a whole block later, with it from 16 MB on.
 constexpr int LN_WAVES = 4;                             // of a workgroup whose teams lie within waves
 struct LnShape {
     int pieces, lanes, waves, v;                        // of a row; lanes 0: WIDE; pieces a lane has
@@ -73,6 +86,25 @@ template <int VEC, bool ODD> __device__ __forceinline__ void ln_put_sums(float *
     }
 }
 
+// Stores piece v of a row.  The overlap of an ODD row's last piece is stored twice with the same bits by one wave.  In a WIDE row the
+// two pieces may lie in different waves, and the output may lie where an input does: a wave that is ahead would overwrite what the
+// other has yet to load.  There each element is stored by the one lane that counts it, and what else that lane has loaded is not used.
+template <class T, int VEC, int V, bool ODD, bool WIDE>
+__device__ __forceinline__ void ln_store(typename Row<T>::elem *row, const LnLane<T, VEC, V, ODD> &at, int v,
+                                         typename Piece<T, VEC, ODD>::raw w, bool past)
+{
+    using P = Piece<T, VEC, ODD>;
+    if constexpr (ODD && WIDE)
+        if (v == V - 1 && at.skip) {
+            const auto parts = __builtin_bit_cast(typename Row<T>::elems, w);
+#pragma unroll
+            for (int e = 1; e < VEC; ++e)
+                if (e >= at.skip) row[at.c0[v] + e] = parts.v[e];
+            return;
+        }
+    P::store(row + at.c0[v], w, past);
+}
+
 // Sums over a row: its team's lanes (FULL: all 64), or the workgroup's waves through red (two arrays used in turn: between two
 // uses of one lies the other's barrier).
 template <bool FULL, bool WIDE, int N> __device__ __forceinline__ void row_sums(float (&v)[N], int lanes, float *red)
@@ -106,7 +138,7 @@ template <bool WIDE> struct LnRows {
 };
 
 template <class T, int VEC, int V, int MODE, bool ODD, bool WIDE, bool FULL>
-__global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_fwd_kernel(const LayerNormArgs p, const LnShape q)
+__global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_kernel(const LayerNormArgs p, const LnShape q)
 {
     constexpr bool JOINED = MODE > 0, RES = MODE > 1;
     using P = Piece<T, VEC, ODD>;
@@ -141,6 +173,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_fwd_ke
     auto row = [&](const Buf &b) {
         const int64_t base = it.row * p.C;
         float f[V][VEC], sum[1] = {0.f}, sq[1] = {0.f};
+        raw out[JOINED ? V : 1];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             P::unpack(b.x[v], f[v]);
@@ -154,15 +187,18 @@ __global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_fwd_ke
                 if constexpr (RES) P::unpack(b.res[v], r);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[v][e] = RES ? fmaf(f[v][e], p.drop.scale, r[e]) : f[v][e] * p.drop.scale;
-                const raw out = P::pack(f[v]);
-                if (at.on[v]) P::store(static_cast<elem *>(p.s) + base + at.c0[v], out, q.past);
-                P::unpack(out, f[v]);
+                out[v] = P::pack(f[v]);
+                P::unpack(out[v], f[v]);
             }
             if (at.on[v])
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) sum[0] += !ODD || v < V - 1 || e >= at.skip ? f[v][e] : 0.f;
         }
         row_sums<FULL, WIDE>(sum, lanes, red[0]);
+        if constexpr (JOINED)                           // behind the sum, which has waited for all of the row: s may lie where x does
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (at.on[v]) ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.s) + base, at, v, out[v], q.past);
         const float mean = sum[0] * inv;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -181,7 +217,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_fwd_ke
         for (int v = 0; v < V; ++v) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) f[v][e] = fmaf(f[v][e] * rstd, gamma[v][e], beta[v][e]);
-            if (at.on[v]) P::store(static_cast<elem *>(p.y) + base + at.c0[v], P::pack(f[v]));
+            if (at.on[v]) ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.y) + base, at, v, P::pack(f[v]), false);
         }
         if (l == 0) {
             if (p.mean) p.mean[it.row] = mean;
@@ -202,13 +238,13 @@ __global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_fwd_ke
 // up e d.  The lanes that hold a channel add up its part of dgamma and dbeta over their rows in registers; at the end the teams of
 // a wave, then the waves of the workgroup are added (fixed order) and the workgroup's sums written as one slab.
 template <class T, int VEC, int V, int MODE, bool ODD, bool WIDE, bool FULL>
-__global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_bwd_kernel(const LayerNormArgs p, const LnShape q)
+__global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_kernel(const LayerNormArgs p, const LnShape q)
 {
     constexpr bool JOINED = MODE > 0, RES = MODE > 1;
     using P = Piece<T, VEC, ODD>;
     using elem = typename P::elem;
     using raw = typename P::raw;
-    constexpr int DEPTH = WIDE && V * VEC <= 8 ? 3 : 2;
+    constexpr int DEPTH = 2;
     extern __shared__ float lds[];                      // WIDE: [2][2][16]; otherwise the sums of the workgroup's waves
     const int lanes = WIDE ? (int)blockDim.x : FULL ? 64 : q.lanes;
     const int l = threadIdx.x & (lanes - 1);
@@ -277,7 +313,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_bwd_ke
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) d[e] += r[e];
                 }
-                if (p.dres) P::store(static_cast<elem *>(p.dres) + base + at.c0[v], P::pack(d), q.past);
+                if (p.dres) ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.dres) + base, at, v, P::pack(d), q.past);
                 if (!p.dx) continue;
                 if (p.drop.t) {
                     uint32_t w[(VEC + 1) / 2];
@@ -287,7 +323,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 64 * LN_WAVES) void layer_norm_bwd_ke
                     for (int e = 0; e < VEC; ++e) d[e] *= p.drop.scale;
                 }
             }
-            P::store(static_cast<elem *>(p.dx) + base + at.c0[v], P::pack(d));
+            ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.dx) + base, at, v, P::pack(d), false);
         }
     };
     for (int64_t k = 0; k < q.trips; k += DEPTH) {
@@ -351,7 +387,8 @@ __device__ __forceinline__ float block_sum(float v, float *red)
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Rows too long for the registers: one row per workgroup, each thread the elements c = thread, thread + 256, ...
+// Rows too long for the registers (more than 16384 16-bit or 8192 fp32 channels): one row per workgroup, each thread the elements
+// c = thread, thread + 256, ...; the later passes over a row find it in the caches.
 template <class T, bool JOINED>
 __global__ __launch_bounds__(LN_THREADS) void layer_norm_long_fwd_kernel(const LayerNormArgs p)
 {
@@ -463,75 +500,85 @@ __global__ __launch_bounds__(LN_THREADS) void layer_norm_param_kernel(const Laye
             (red[wave][0][lane] + red[wave][1][lane]) + (red[wave][2][lane] + red[wave][3][lane]);
 }
 
-// dgamma and dbeta from the slabs' sums: 16 columns a workgroup, 64 lanes down the slabs, then a tree.
+// dgamma and dbeta from the slabs' sums: a workgroup has 16 columns and 64 lanes down the slabs, four of them in a wave.  With U >=
+// slabs / 64 all loads go out at once: the kernel is one trip to memory, two lane exchanges, one barrier.
+template <int U>
 __global__ __launch_bounds__(1024) void layer_norm_param_sum_kernel(const float *partial, int slabs, int C, float *dgamma, float *dbeta)
 {
-    __shared__ float red[64][17];
-    const int col = threadIdx.x & 15, lane = threadIdx.x >> 4;
+    __shared__ float red[16][16];
+    const int col = threadIdx.x & 15, lane = threadIdx.x >> 4, wave = threadIdx.x >> 6;
     const int64_t i = (int64_t)blockIdx.x * 16 + col, all = 2 * (int64_t)C;
-    float sum = 0.f;
-    for (int z0 = 0; z0 < slabs; z0 += 64 * 16) {       // all loads of up to 1024 slabs at once: the kernel is one trip to memory
-        float f[16];
+    float f[U];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            const int z = z0 + 64 * u + lane;
-            f[u] = z < slabs && i < all ? partial[z * all + i] : 0.f;
-        }
-#pragma unroll
-        for (int half = 8; half > 0; half >>= 1)
-#pragma unroll
-            for (int u = 0; u < half; ++u) f[u] += f[u + half];
-        sum += f[0];
+    for (int u = 0; u < U; ++u) {
+        const int z = 64 * u + lane;
+        f[u] = z < slabs && i < all ? partial[z * all + i] : 0.f;
     }
-    red[lane][col] = sum;
+#pragma unroll
+    for (int u = 1; u < U; ++u) f[0] += f[u];
+    const float sum = swap32_add(swap16_add(f[0]));
+    if ((threadIdx.x & 63) < 16) red[wave][col] = sum;
     __syncthreads();
+    if (threadIdx.x < 16 && i < all) {
+        float s = red[0][col];
 #pragma unroll
-    for (int half = 32; half > 0; half >>= 1) {
-        if (lane < half) red[lane][col] += red[lane + half][col];
-        __syncthreads();
+        for (int w = 1; w < 16; ++w) s += red[w][col];
+        (i < C ? dgamma[i] : dbeta[i - C]) = s;
     }
-    if (lane == 0 && i < all) (i < C ? dgamma[i] : dbeta[i - C]) = red[0][col];
 }
 
 // ---- dispatch ----------------------------------------------------------------
 constexpr int CUS = 256;
 static int pow2_from(int v) { int p = 1; while (p < v) p <<= 1; return p; }
 
-// Up to 2048 pieces of a row stay in the registers of 16 waves.
+// Up to 2048 pieces of a row stay in the registers of 8 waves.
 template <class T> static bool ln_long(int C) { return C > 2048 * Row<T>::E; }
 
 template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd)
 {
     constexpr int E = Row<T>::E;
+    // The figures are bf16 rows, 64 M elements where no other size is given; forward first.
+    const bool large = n * C * (16 / E) >= 64 << 20;
     LnShape q{};
     q.waves = LN_WAVES;
     q.v = 1;
     q.pieces = C < E ? C : (C + E - 1) / E;
     q.past = C >= E && n * C * (16 / E) >= 16 << 20;
-    if (q.pieces <= 8 || C < E) q.lanes = pow2_from(q.pieces);
-    else if (q.pieces <= 192) {
-        // the number of pieces a lane that leaves fewest lanes idle, 8 lanes (a 128-byte line) at least
-        const int first = bwd && q.pieces < 32 ? 1 : 2;
-        int best = 1 << 30;
-        for (int v : {first, 3 - first, 3}) {
-            const int lanes = std::max(8, pow2_from((q.pieces + v - 1) / v));
-            if (lanes <= 64 && lanes * v < best) {
-                best = lanes * v;
-                q.lanes = lanes;
-                q.v = v;
+    int64_t most;                                       // workgroups
+    if (q.pieces <= 192) {
+        if (q.pieces <= 8) q.lanes = pow2_from(q.pieces);
+        else {
+            // The number of pieces a lane that leaves fewest lanes idle, 8 lanes (a 128-byte line) at least: 304 channels 52.9 us with
+            // three pieces (48 places for 38), 61.4 with two (64 places); 64 channels 50.0 with one, 54.5 with two and 4 lanes.
+            // Where one and two leave the same, two: 256 channels 47.7 and 49.6.  The backward pass has one on short rows (96
+            // channels 71.9, with two 82.7).
+            const int first = bwd && q.pieces < 32 ? 1 : 2;
+            int best = 1 << 30;
+            for (int v : {first, 3 - first, 3}) {
+                const int lanes = std::max(8, pow2_from((q.pieces + v - 1) / v));
+                if (lanes <= 64 && lanes * v < best) {
+                    best = lanes * v;
+                    q.lanes = lanes;
+                    q.v = v;
+                }
             }
         }
+        // Loads under way, not more: from 64 MB on 8 waves a compute unit with two or three pieces a lane, 16 with one (1769472 x 256
+        // fp16 318 us with 8 waves, 367 with 16: fewer rows at a time stay within fewer memory pages); twice that on smaller tensors,
+        // where a wave has few rows (8192 x 1024 9.0 us, 9.4 with half).  Backward, where each workgroup's sums are a slab of the
+        // workspace, half as many: 256 slabs with two pieces or more (65536 x 1024 67.9 us, 70.6 with 512), 768 with one (96 channels
+        // 71.9, with 256 116).
+        most = bwd ? (q.v == 1 ? 3 : 1) * CUS : (q.v == 1 ? 8 : 4) * CUS / (large ? 2 : 1);
     } else {
-        // two sums of a 16-bit piece's channels and the rows under way are half of a wave's registers: one piece a lane
-        const int most = bwd && E == 8 ? 64 : 128;
-        q.waves = std::min(16, std::max(LN_WAVES, pow2_from((q.pieces + most - 1) / most)));
+        // As few waves a row as its registers allow, since they wait for each other at two barriers (one, backward): up to four
+        // pieces a lane (fp16 8192 x 4096 27.6 us with 2 waves, 29.8 with 4, 48.6 with 8), two in the backward pass, which holds
+        // the sums of its channels too (44.0 us with 4 waves, 51.9 with 8, 55.0 with 2).  8 waves a compute unit; with one piece a
+        // lane and many rows 12 (20971 x 1600 44.7 us, 51.2 with 8; 2048 x 2048 17.7 with 12, 13.9 with 8).
+        q.waves = std::min(8, bwd ? std::max(4, pow2_from((q.pieces + 127) / 128)) : pow2_from((q.pieces + 255) / 256));
         q.v = (q.pieces + 64 * q.waves - 1) / (64 * q.waves);
+        most = (bwd && q.v == 1 && n >= 16384 ? 12 : 8) * CUS / q.waves;
     }
     const int64_t per = q.lanes ? 64 * LN_WAVES / q.lanes : 1, want = (n + per - 1) / per;
-    int64_t most;
-    if (bwd) most = q.lanes ? (q.v == 1 ? 3 : 1) * CUS : q.v == 1 && q.waves == LN_WAVES ? 2 * CUS : CUS;
-    else if (q.lanes) most = (q.v == 1 ? 8 : 4) * CUS / (n * C * (16 / E) >= 64 << 20 ? 2 : 1);
-    else most = (q.v == 1 ? 8 : 4) * CUS * LN_WAVES / q.waves;
     q.grid = (int)std::max<int64_t>(1, std::min(want, most));
     q.trips = (want + q.grid - 1) / q.grid;
     return q;
@@ -555,7 +602,7 @@ static void ln_launch(const LayerNormArgs &a, const LnShape &q, bool bwd, hipStr
         constexpr int MODE = decltype(mode)::value;
         constexpr bool ODD = decltype(odd)::value;
         if (bwd) DLK_LAUNCH("layer_norm_bwd_kernel", (layer_norm_bwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, lds, stream, a, q);
-        else DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, 0, stream, a, q);
+        else if constexpr (!WIDE || V > 1) DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, 0, stream, a, q);
     };
     const auto mode = [&](auto odd) {
         if (!a.joined) go(std::integral_constant<int, 0>{}, odd);
@@ -579,7 +626,9 @@ static hipError_t ln_resident(const LayerNormArgs &a, const LnShape &q, bool bwd
     else if (q.lanes && q.v == 2) ln_launch<T, E, 2, false, false>(a, q, bwd, stream);
     else if (q.lanes) ln_launch<T, E, 3, false, false>(a, q, bwd, stream);
     else if (q.v == 1) ln_launch<T, E, 1, true, false>(a, q, bwd, stream);
-    else ln_launch<T, E, 2, true, false>(a, q, bwd, stream);
+    else if (q.v == 2) ln_launch<T, E, 2, true, false>(a, q, bwd, stream);
+    else if (q.v == 3) ln_launch<T, E, 3, true, false>(a, q, bwd, stream);
+    else ln_launch<T, E, 4, true, false>(a, q, bwd, stream);
     return launch_status();
 }
 
@@ -602,7 +651,9 @@ hipError_t launch_layer_norm_fwd(const LayerNormArgs &a, int dtype, hipStream_t 
 static hipError_t ln_param_sum(const LayerNormArgs &a, int slabs, hipStream_t stream)
 {
     const dim3 grid((unsigned)((2 * (int64_t)a.C + 15) / 16)), block(1024);
-    DLK_LAUNCH("layer_norm_param_sum_kernel", layer_norm_param_sum_kernel, grid, block, 0, stream, a.partial, slabs, a.C, a.dgamma, a.dbeta);
+    static_assert(3 * CUS <= 64 * 12, "the longest list of slabs");
+    if (slabs <= 256) DLK_LAUNCH("layer_norm_param_sum_kernel", layer_norm_param_sum_kernel<4>, grid, block, 0, stream, a.partial, slabs, a.C, a.dgamma, a.dbeta);
+    else DLK_LAUNCH("layer_norm_param_sum_kernel", layer_norm_param_sum_kernel<12>, grid, block, 0, stream, a.partial, slabs, a.C, a.dgamma, a.dbeta);
     return launch_status();
 }
 

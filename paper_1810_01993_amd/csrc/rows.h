@@ -24,6 +24,7 @@ __device__ __forceinline__ float settled(float v)
 template <class T> struct Row {                        // 16-bit storage
     using elem = uint16_t;
     static constexpr int E = 8;                        // elements of a 16-byte piece
+    struct elems { elem v[E]; };
     static __device__ __forceinline__ float get(elem v) { return T::to_float(v); }
     static __device__ __forceinline__ elem put(float v) { return T::from_float(settled(v)); }
     static __device__ __forceinline__ void unpack(u32x4_t w, float (&v)[E])
@@ -45,6 +46,7 @@ template <class T> struct Row {                        // 16-bit storage
 template <> struct Row<F32> {
     using elem = float;
     static constexpr int E = 4;
+    struct elems { elem v[E]; };
     static __device__ __forceinline__ float get(elem v) { return v; }
     static __device__ __forceinline__ elem put(float v) { return v; }
     static __device__ __forceinline__ void unpack(u32x4_t w, float (&v)[E])

@@ -91,7 +91,8 @@ def _joined(api, n, C, dtype, p=0.2, residual=True, stream=True, affine=True):
 SHAPES = [(1, 1), (3, 2), (9, 3), (700, 5), (1, 7), (5, 8), (33, 9), (257, 16), (64, 24), (101, 31), (77, 33), (66, 48), (130, 64),
           (19, 65), (4099, 77), (31, 100), (9, 127), (8, 255), (2, 256), (1031, 256), (4, 257), (999, 304), (35, 511), (3, 512),
           (5, 513), (61, 771), (130, 1024), (7, 1025), (17, 2047), (21, 2048), (6, 2049), (3, 2056), (2, 3001), (5, 4096),
-          (3, 4097), (4, 8192), (2, 8193), (3, 8200), (1, 12345), (2, 16384), (2, 16385), (1, 40000)]
+          (3, 4097), (4, 8192), (2, 8193), (3, 8200), (1, 12345), (2, 12289), (2, 16384), (2, 16385), (1, 40000),
+          (40, 768), (41, 769), (20, 1536), (21, 1537), (700, 2057)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -116,6 +117,13 @@ MANY = [(20011, 8), (30011, 24), (100003, 3), (25013, 40), (65537, 64), (20001, 
 def test_many_rows(api, n, C, dtype):
     _alone(api, n, C, dtype)
     _joined(api, n, C, dtype)
+
+
+@pytest.mark.parametrize("dtype,C", [("f16", 1544), ("f32", 772)])
+def test_many_rows_of_one_piece_a_lane(api, dtype, C):
+    """A workgroup per row with one piece a lane, either side of the row count from which more workgroups share the rows."""
+    for n in (16383, 16384):
+        _alone(api, n, C, dtype)
 
 
 @pytest.mark.parametrize("n,C", [(2 * 48 * 72, 1024), (2 * 192 * 288, 304)])
@@ -167,7 +175,7 @@ def test_a_bad_row_stays_alone(api, C, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("n,C", [(65, 48), (65, 77), (300, 256), (9, 2048), (5, 4100), (3, 9001), (2, 20001)])
+@pytest.mark.parametrize("n,C", [(65, 48), (65, 77), (300, 256), (9, 2048), (5, 4100), (3, 9001), (2, 20001), (900, 1801), (700, 4099)])
 def test_in_place_and_repeatable(api, n, C, dtype):
     """Outputs over inputs, as the header allows, and the same bits from the same call."""
     x, res, dy, ds = (_rand((n, C), dtype, C + k) for k in range(4))
