@@ -222,7 +222,8 @@ dl_status dropout_bwd(const void *dy, const dl_dropout *dropout, int32_t dtype, 
  * F32),
  *   m = sum_c x[c] / C;  v = sum_c (x[c] - m)^2 / C;  r = 1 / sqrt(v + eps)
  *   y[c] = (x[c] - m) * r * gamma[c] + beta[c]
- * in fp32, rounded once.  gamma, beta: device float[C], or both NULL (1 and 0).
+ * in fp32 (values whose squared distance from the mean passes fp32's range, about
+ * 1e19, give r = 0), rounded once.  gamma, beta: device float[C], or both NULL (1 and 0).
  * mean, rstd: device float[n_pixels], what the backward pass takes, or NULL (not
  * written; inference).  eps finite and >= 0 (with 0 a row of equal values has
  * no finite r): DL_ERR_VALUE otherwise.  1 <= C <= DL_NORM_MAX_CHANNELS,

@@ -227,6 +227,22 @@ def test_outputs_left_out(api):
     assert torch.equal(y2, y)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,C", [(33, 77), (5, 2048)])
+def test_everything_dropped(api, n, C, dtype):
+    """p = 1 over infinities and NaN: without a residual every row of s is empty (zero), y is beta and no gradient reaches x."""
+    x = torch.full((n, C), float("nan"), device="cuda").to(M.DT[dtype])
+    x[::2] = float("inf")
+    gamma, beta, d = _vec(C, 1, 1.0), _vec(C, 2), api.DropoutDesc(1.0, 7)
+    s, y, m, r = api.dropout_add_layer_norm_fwd(x, None, d, gamma, beta)
+    assert not s.any() and not m.any() and torch.equal(y, beta.to(M.DT[dtype]).expand(n, C))
+    M.assert_within(r, np.full(n, float(np.float32(1e-5)) ** -0.5), np.full(n, 4 * M.U32 * 317), "rstd")     # a square root and a division
+    dy, ds = _rand((n, C), dtype, 1), _rand((n, C), dtype, 2)
+    dres, dx, dg, db = api.dropout_add_layer_norm_bwd(dy, ds, s, d, gamma, m, r)
+    assert not dx.any() and not dg.any()
+    M.check_backward(dy, s, gamma, m, r, dres, dg, db, dtype, ds)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_gradients_against_differences(api, dtype):
     """dx, dgamma and dbeta against central differences of the oracle's forward pass at the stored inputs."""
