@@ -207,6 +207,32 @@ def test_in_place_and_repeatable(api, n, C, dtype):
     assert all(torch.equal(p, q) for p, q in zip(both, api.dropout_add_layer_norm_fwd(x, x.clone(), d, gamma, beta)))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,C", [(40, 200), (300, 77), (6, 2600), (3, 20001)])
+def test_least_alignment(api, n, C, dtype):
+    """Tensors that begin 16 bytes into a line, float arrays 4 bytes: the same bits as from a fresh allocation."""
+    step = 16 // M.DT[dtype].itemsize
+
+    def moved(t, by):
+        buf = torch.zeros(t.numel() + by, dtype=t.dtype, device="cuda")
+        buf[by:] = t.reshape(-1)
+        return buf[by:].view(t.shape)
+    x, res, dy, ds = (_rand((n, C), dtype, C + k) for k in range(4))
+    gamma, beta, d = _vec(C, 1, 1.0), _vec(C, 2), api.DropoutDesc(0.25, 3, 4)
+    want = api.dropout_add_layer_norm_fwd(x, res, d, gamma, beta)
+    outs = [moved(t, by) for t, by in zip(want, (step, 3 * step, 1, 3))]
+    got = api.dropout_add_layer_norm_fwd(moved(x, step), moved(res, 5 * step), d, moved(gamma, 1), moved(beta, 3), s=outs[0], y=outs[1],
+                                         mean=outs[2], rstd=outs[3])
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    s, _, m, r = want
+    want = api.dropout_add_layer_norm_bwd(dy, ds, s, d, gamma, m, r)
+    outs = [moved(t, by) for t, by in zip(want, (step, 7 * step, 1, 2))]
+    ws = torch.empty(api.dl_layer_norm_bwd_workspace_bytes(n, C) + 16, dtype=torch.uint8, device="cuda")[16:]
+    got = api.dropout_add_layer_norm_bwd(moved(dy, step), moved(ds, 3 * step), moved(s, step), d, moved(gamma, 1), moved(m, 1), moved(r, 3),
+                                         dresidual=outs[0], dx=outs[1], dgamma=outs[2], dbeta=outs[3], workspace=ws)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
 def test_outputs_left_out(api):
     """The C boundary writes only what it is given: dx or dresidual alone, statistics left out."""
     n, C = 70, 77
