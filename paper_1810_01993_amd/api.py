@@ -441,46 +441,42 @@ def bias_relu_bwd(dy: torch.Tensor, y: torch.Tensor | None, relu: bool, dz: torc
 
 
 _ROW_DTYPES = {torch.float16: DL_F16, torch.bfloat16: DL_BF16, torch.float32: DL_F32}
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _begin(x: torch.Tensor):
-    """(dtype code, current stream) of a call on a [..., channels] operand, which has to lie on the current device."""
-    code = _ROW_DTYPES.get(x.dtype)
+def _operands(names: str, x: torch.Tensor, *tensors):
+    """(dtype code, current stream, device index, x's shape, addresses) of a call on x and operands that match it (None for one that
+    is left out); x has to lie on the current device.  One pass, with what x has looked up once: the attributes of a tensor take
+    longer than the arithmetic of a small call."""
+    dtype, shape, index = x.dtype, x.shape, x.get_device()
+    code = _ROW_DTYPES.get(dtype)
     if code is None:
-        raise TypeError(f"fp16, bf16 or fp32 tensor required, got {x.dtype}")
-    index = x.get_device()
-    if index < 0:
+        raise TypeError(f"fp16, bf16 or fp32 tensor required, got {dtype}")
+    if index < 0 or not x.is_contiguous():
         raise ValueError("contiguous device tensor required")
-    if index != torch._C._cuda_getDevice():
+    if index != _current_device():
         raise ValueError("the tensors must lie on the current device")
-    return code, torch._C._cuda_getCurrentRawStream(index)
-
-
-def _like(names: str, ref: torch.Tensor, *tensors):
-    """The addresses of operands that match ref (None for one that is left out).  One pass with what ref is looked up once: the
-    attributes of a tensor take longer than the arithmetic of a small call."""
-    dtype, shape, index = ref.dtype, ref.shape, ref.get_device()
-    out = []
+    out = [x.data_ptr()]
     for t in tensors:
         if t is None:
             out.append(None)
-            continue
-        if (t is not ref and (t.dtype is not dtype or t.shape != shape or t.get_device() != index)) or not t.is_contiguous():
-            raise ValueError(f"{names.split()[len(out)]}: contiguous {dtype} tensor of shape {tuple(shape)} on {ref.device} required")
-        out.append(t.data_ptr())
-    return out
+        elif t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            raise ValueError(f"{names.split()[len(out) - 1]}: contiguous {dtype} tensor of shape {tuple(shape)} on {x.device} required")
+    return code, _raw_stream(index), index, shape, out
 
 
-def _vectors(names: str, ref: torch.Tensor, count: int, *tensors):
-    """The addresses of float32 arrays of count elements on ref's device (None for one that is left out)."""
-    f32, index, out = torch.float32, ref.get_device(), []
+def _vectors(names: str, index: int, count: int, *tensors):
+    """The addresses of float32 arrays of count elements on a device (None for one that is left out)."""
+    f32, out = torch.float32, []
     for t in tensors:
         if t is None:
             out.append(None)
-            continue
-        if t.dtype is not f32 or t.numel() != count or t.get_device() != index or not t.is_contiguous():
-            raise ValueError(f"{names.split()[len(out)]}: contiguous float32 tensor of {count} elements on {ref.device} required")
-        out.append(t.data_ptr())
+        elif t.dtype is f32 and t.numel() == count and t.get_device() == index and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            raise ValueError(f"{names.split()[len(out)]}: contiguous float32 tensor of {count} elements on device {index} required")
     return out
 
 
@@ -488,7 +484,7 @@ def _drop(dropout: DropoutDesc | None, x: torch.Tensor):
     """The C structure of a dropout descriptor whose step, if any, lies where the tensors do."""
     if dropout is None:
         return None
-    if dropout.step is not None and dropout.step.device != x.device:
+    if dropout.step is not None and dropout.step.get_device() != x.get_device():
         raise ValueError("step must lie on the tensors' device")
     return dropout._kept
 
@@ -496,45 +492,42 @@ def _drop(dropout: DropoutDesc | None, x: torch.Tensor):
 def dropout_fwd(x: torch.Tensor, dropout: DropoutDesc, residual: torch.Tensor | None = None,
                 y: torch.Tensor | None = None) -> torch.Tensor:
     """y = residual + (kept ? scale * x : 0) with the mask that ``dropout`` names; x fp16, bf16 or fp32 of any shape."""
-    code, stream = _begin(x)
     if y is None:
         y = torch.empty_like(x)
-    xp, rp, yp = _like("x residual y", x, x, residual, y)
+    code, stream, _, _, (xp, rp, yp) = _operands("residual y", x, residual, y)
     _check(_lib.dropout_fwd(xp, rp, _drop(dropout, x), code, x.numel(), yp, stream), "dropout_fwd")
     return y
 
 
 def dropout_bwd(dy: torch.Tensor, dropout: DropoutDesc, dx: torch.Tensor | None = None) -> torch.Tensor:
     """dx = kept ? scale * dy : 0 with the forward call's mask (the residual's gradient is dy itself)."""
-    code, stream = _begin(dy)
     if dx is None:
         dx = torch.empty_like(dy)
-    gp, xp = _like("dy dx", dy, dy, dx)
+    code, stream, _, _, (gp, xp) = _operands("dx", dy, dx)
     _check(_lib.dropout_bwd(gp, _drop(dropout, dy), code, dy.numel(), xp, stream), "dropout_bwd")
     return dx
 
 
-def _rows(x: torch.Tensor):
+def _rows(x: torch.Tensor, shape):
     """(pixels, channels) of a [..., C] tensor."""
-    shape = x.shape
     if not shape or shape[-1] < 1:
         raise ValueError("[..., C] tensor with C >= 1 required")
     return x.numel() // shape[-1], shape[-1]
 
 
-def _affine(gamma, beta, x, C):
+def _affine(gamma, beta, index, C):
     if (gamma is None) != (beta is None):
         raise ValueError("gamma and beta: both or neither")
-    return _vectors("gamma beta", x, C, gamma, beta)
+    return _vectors("gamma beta", index, C, gamma, beta)
 
 
-def _stats_out(x, n, mean, rstd, want_stats):
-    if want_stats:
-        if mean is None:
-            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        if rstd is None:
-            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    return mean, rstd, *_vectors("mean rstd", x, n, mean, rstd)
+def _new_stats(x, mean, rstd):
+    """The statistics' tensors, new where none is given."""
+    if mean is None:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    return mean, rstd
 
 
 def layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tensor | None, eps: float = 1e-5,
@@ -542,13 +535,14 @@ def layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tens
                    want_stats: bool = True):
     """Layer norm over the last dimension: x [..., C] fp16, bf16 or fp32, gamma and beta float32[C] (or both None).  Returns
     (y, mean, rstd); the float32 statistics [...] are for layer_norm_bwd (None with want_stats False: inference)."""
-    code, stream = _begin(x)
-    n, C = _rows(x)
-    g, b = _affine(gamma, beta, x, C)
     if y is None:
         y = torch.empty_like(x)
-    mean, rstd, m, r = _stats_out(x, n, mean, rstd, want_stats)
-    xp, yp = _like("x y", x, x, y)
+    code, stream, index, shape, (xp, yp) = _operands("y", x, y)
+    n, C = _rows(x, shape)
+    g, b = _affine(gamma, beta, index, C)
+    if want_stats:
+        mean, rstd = _new_stats(x, mean, rstd)
+    m, r = _vectors("mean rstd", index, n, mean, rstd)
     _check(_lib.layer_norm_fwd(xp, g, b, code, n, C, eps, yp, m, r, stream), "layer_norm_fwd")
     return y, mean, rstd
 
@@ -559,7 +553,7 @@ def dl_layer_norm_bwd_workspace_bytes(n_pixels: int, C: int) -> int:
     return need.value
 
 
-def _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params):
+def _param_grads(dy, index, n, C, dgamma, dbeta, workspace, want_params):
     """(dgamma, dbeta, their addresses, the workspace's and its bytes, the workspace) of a backward call."""
     if not want_params:
         return None, None, None, None, None, 0, None
@@ -569,9 +563,9 @@ def _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params):
         dbeta = torch.empty(C, dtype=torch.float32, device=dy.device)
     if workspace is None:
         workspace = torch.empty(dl_layer_norm_bwd_workspace_bytes(n, C), dtype=torch.uint8, device=dy.device)
-    elif workspace.get_device() != dy.get_device() or not workspace.is_contiguous():
+    elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError(f"workspace: contiguous tensor on {dy.device} required")
-    dg, db = _vectors("dgamma dbeta", dy, C, dgamma, dbeta)
+    dg, db = _vectors("dgamma dbeta", index, C, dgamma, dbeta)
     return dgamma, dbeta, dg, db, workspace.data_ptr(), workspace.nbytes, workspace
 
 
@@ -580,14 +574,13 @@ def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None
                    workspace: torch.Tensor | None = None, want_params: bool = True):
     """Gradients of layer_norm_fwd from dy, its input x and its statistics.  Returns (dx, dgamma float32[C], dbeta float32[C]);
     with want_params False the last two are None and no workspace is needed."""
-    code, stream = _begin(dy)
-    n, C = _rows(dy)
     if dx is None:
         dx = torch.empty_like(dy)
-    dgamma, dbeta, dg, db, wp, nb, workspace = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
-    gp, xp, dp = _like("dy x dx", dy, dy, x, dx)
-    (ga,) = _vectors("gamma", dy, C, gamma)
-    m, r = _vectors("mean rstd", dy, n, mean, rstd)
+    code, stream, index, shape, (gp, xp, dp) = _operands("x dx", dy, x, dx)
+    n, C = _rows(dy, shape)
+    dgamma, dbeta, dg, db, wp, nb, workspace = _param_grads(dy, index, n, C, dgamma, dbeta, workspace, want_params)
+    (ga,) = _vectors("gamma", index, C, gamma)
+    m, r = _vectors("mean rstd", index, n, mean, rstd)
     _check(_lib.layer_norm_bwd(gp, xp, ga, m, r, code, n, C, dp, dg, db, wp, nb, stream), "layer_norm_bwd")
     return dx, dgamma, dbeta
 
@@ -598,15 +591,16 @@ def dropout_add_layer_norm_fwd(x: torch.Tensor, residual: torch.Tensor | None, d
                                rstd: torch.Tensor | None = None, want_stats: bool = True):
     """s = residual + dropout(x), y = layer_norm(s) in one pass, with the bits of the two calls.  residual None: none; dropout
     None: nothing is dropped.  Returns (s, y, mean, rstd)."""
-    code, stream = _begin(x)
-    n, C = _rows(x)
-    g, b = _affine(gamma, beta, x, C)
     if s is None:
         s = torch.empty_like(x)
     if y is None:
         y = torch.empty_like(x)
-    mean, rstd, m, r = _stats_out(x, n, mean, rstd, want_stats)
-    xp, rp, sp, yp = _like("x residual s y", x, x, residual, s, y)
+    code, stream, index, shape, (xp, rp, sp, yp) = _operands("residual s y", x, residual, s, y)
+    n, C = _rows(x, shape)
+    g, b = _affine(gamma, beta, index, C)
+    if want_stats:
+        mean, rstd = _new_stats(x, mean, rstd)
+    m, r = _vectors("mean rstd", index, n, mean, rstd)
     _check(_lib.dropout_add_layer_norm_fwd(xp, rp, _drop(dropout, x), g, b, code, n, C, eps, sp, yp, m, r, stream),
            "dropout_add_layer_norm_fwd")
     return s, y, mean, rstd
@@ -619,16 +613,15 @@ def dropout_add_layer_norm_bwd(dy: torch.Tensor, ds: torch.Tensor | None, s: tor
                                workspace: torch.Tensor | None = None, want_params: bool = True):
     """Gradients of dropout_add_layer_norm_fwd: dy reaches y, ds (or None) reaches s by the residual stream.  Returns
     (dresidual, dx, dgamma, dbeta); the last two are None with want_params False."""
-    code, stream = _begin(dy)
-    n, C = _rows(dy)
     if dresidual is None:
         dresidual = torch.empty_like(dy)
     if dx is None:
         dx = torch.empty_like(dy)
-    dgamma, dbeta, dg, db, wp, nb, workspace = _param_grads(dy, n, C, dgamma, dbeta, workspace, want_params)
-    gp, sg, sp, rp, dp = _like("dy ds s dresidual dx", dy, dy, ds, s, dresidual, dx)
-    (ga,) = _vectors("gamma", dy, C, gamma)
-    m, r = _vectors("mean rstd", dy, n, mean, rstd)
+    code, stream, index, shape, (gp, sg, sp, rp, dp) = _operands("ds s dresidual dx", dy, ds, s, dresidual, dx)
+    n, C = _rows(dy, shape)
+    dgamma, dbeta, dg, db, wp, nb, workspace = _param_grads(dy, index, n, C, dgamma, dbeta, workspace, want_params)
+    (ga,) = _vectors("gamma", index, C, gamma)
+    m, r = _vectors("mean rstd", index, n, mean, rstd)
     _check(_lib.dropout_add_layer_norm_bwd(gp, sg, sp, _drop(dropout, dy), ga, m, r, code, n, C, rp, dp, dg, db, wp, nb, stream),
            "dropout_add_layer_norm_bwd")
     return dresidual, dx, dgamma, dbeta

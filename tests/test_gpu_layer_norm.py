@@ -389,7 +389,8 @@ def test_refusals_on_the_device(api):
     x, v = torch.zeros((6, 8), dtype=torch.float16, device="cuda"), torch.zeros(8, device="cuda")
     m = torch.zeros(6, device="cuda")
     for call in (lambda: api.layer_norm_fwd(x.t(), v[:6], v[:6]), lambda: api.layer_norm_fwd(x, v, v[:4]), lambda: api.layer_norm_fwd(x, v, None),
-                 lambda: api.layer_norm_fwd(x, v.half(), v.half()), lambda: api.layer_norm_fwd(x, v, v, y=x.float()),
+                 lambda: api.layer_norm_fwd(x, v.half(), v.half()), lambda: api.layer_norm_fwd(x, v, v, y=x.float()), lambda: api.layer_norm_fwd(x, v, v, y=x[:3]),
+                 lambda: api.layer_norm_fwd(x, v, v, y=x.cpu()), lambda: api.layer_norm_fwd(x, v, v, y=x.view(2, 24)),
                  lambda: api.layer_norm_fwd(x, v.cpu(), v.cpu()), lambda: api.layer_norm_bwd(x, x, v, m[:5], m),
                  lambda: api.layer_norm_bwd(x, x.float(), v, m, m), lambda: api.dropout_fwd(x, api.DropoutDesc(0.1, 1), residual=x[:3]),
                  lambda: api.layer_norm_fwd(x[:, :4], v[:4], v[:4])):

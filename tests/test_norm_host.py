@@ -122,15 +122,14 @@ def test_wrapper_refusals(api):
         api.layer_norm_fwd(x.double(), v, v)
     for t in (torch.zeros(()), torch.zeros(3, 0)):
         with pytest.raises(ValueError):
-            api._rows(t)
-    for bad in (x.float(), x[:3], x.t().contiguous().t()):
-        with pytest.raises(ValueError):
-            api._like("x y", x, x, bad)
+            api._rows(t, t.shape)
+    assert api._rows(x, x.shape) == (4, 8)
     for bad in (v.half(), v[:7], torch.zeros(16)[::2]):
         with pytest.raises(ValueError):
-            api._vectors("gamma", v, 8, bad)
+            api._vectors("gamma", -1, 8, bad)
+    assert api._vectors("gamma beta", -1, 8, v, None) == [v.data_ptr(), None]
     with pytest.raises(ValueError):
-        api._affine(v, None, v, 8)
+        api._affine(v, None, -1, 8)
 
 
 def test_host_path_under_sanitizers(tmp_path):
