@@ -226,7 +226,8 @@ dl_status dropout_bwd(const void *dy, const dl_dropout *dropout, int32_t dtype, 
  * 1e19, give r = 0), rounded once.  gamma, beta: device float[C], or both NULL (1 and 0).
  * mean, rstd: device float[n_pixels], what the backward pass takes, or NULL (not
  * written; inference).  eps finite and >= 0 (with 0 a row of equal values has
- * no finite r): DL_ERR_VALUE otherwise.  1 <= C <= DL_NORM_MAX_CHANNELS,
+ * no finite r, and one whose variance lies below 1e-38 no finite gradient):
+ * DL_ERR_VALUE otherwise.  1 <= C <= DL_NORM_MAX_CHANNELS,
  * n_pixels * C < 2^46.  y may be x.  float arrays need 4-byte alignment. */
 #define DL_NORM_MAX_CHANNELS 1048576
 dl_status layer_norm_fwd(const void *x, const float *gamma, const float *beta, int32_t dtype, int64_t n_pixels,

@@ -605,7 +605,7 @@ static void ln_launch(const LayerNormArgs &a, const LnShape &q, bool bwd, hipStr
         constexpr int MODE = decltype(mode)::value;
         constexpr bool ODD = decltype(odd)::value;
         if (bwd) DLK_LAUNCH("layer_norm_bwd_kernel", (layer_norm_bwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, lds, stream, a, q);
-        else if constexpr (!WIDE || V > 1) DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, 0, stream, a, q);
+        else if constexpr (!WIDE || V > 2) DLK_LAUNCH("layer_norm_fwd_kernel", (layer_norm_fwd_kernel<T, VEC, V, MODE, ODD, WIDE, FULL>), grid, block, 0, stream, a, q);
     };
     const auto mode = [&](auto odd) {
         if (!a.joined) go(std::integral_constant<int, 0>{}, odd);
@@ -617,12 +617,13 @@ static void ln_launch(const LayerNormArgs &a, const LnShape &q, bool bwd, hipStr
     mode(std::false_type{});
 }
 
+// (One piece a lane never fills a wave's 64 lanes: two with half of them leave as few idle.  Rows of several waves have three or four
+// pieces a lane in the forward pass.)
 template <class T>
 static hipError_t ln_resident(const LayerNormArgs &a, const LnShape &q, bool bwd, hipStream_t stream)
 {
     constexpr int E = Row<T>::E;
     if (a.C < E) ln_launch<T, 1, 1, false, false>(a, q, bwd, stream);
-    else if (q.lanes == 64 && q.v == 1) ln_launch<T, E, 1, false, true>(a, q, bwd, stream);
     else if (q.lanes == 64 && q.v == 2) ln_launch<T, E, 2, false, true>(a, q, bwd, stream);
     else if (q.lanes == 64) ln_launch<T, E, 3, false, true>(a, q, bwd, stream);
     else if (q.lanes && q.v == 1) ln_launch<T, E, 1, false, false>(a, q, bwd, stream);
