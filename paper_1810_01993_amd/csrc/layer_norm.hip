@@ -11,7 +11,7 @@
 // parameter gradients stay in registers too.  Measured, with the bandwidth of what has to cross (a large copy reaches 5.5-5.7 TB/s):
 //   forward   1769472 x 256 fp16 316 us (5.7 TB/s), 6912 x 1024 bf16 8.1 us (3.5)
 //   backward  110592 x 304 fp16 39 us (5.1), 6912 x 2048 fp32 34 us (5.0), 208297 x 77 bf16 29 us (3.4: rows at odd addresses)
-//   joined    forward 110592 x 256 bf16 43 us (5.2), backward 442368 x 256 bf16 199 us (5.7), 3015 x 512 fp16 11 us (1.4: two
+//   joined    forward 110592 x 256 bf16 38 us (6.0), backward 442368 x 256 bf16 197 us (5.8), 3015 x 512 fp16 10.5 us (1.5: two
 //             launches, 8 and 3 us on their own)
 // Of a backward call about 4.7 us are the second launch, which adds the workgroups' sums in a fixed order.
 #include <algorithm>
@@ -30,13 +30,15 @@ namespace dlk {
 // Rows that are no whole number of pieces (ODD) end in a piece that reaches back over what the one before it covers: the elements
 // that both hold are counted once and stored twice, with the same bits.  VEC = 1: rows shorter than a piece.
 //
-// Loads of whole pieces carry the hint that nobody reads the line again (backward 110592 x 256 fp16: 35.1 us with it, 38.1
-// without); a line that rows share does not.  y and dx are stored without it, the next kernel reads them; s and the residual's
-// gradient, which come back a whole block later, with it from 16 MB on.
+// Whole pieces are loaded with the hint that nobody reads the line again (backward 110592 x 256 fp16: 35.1 us with it, 38.1
+// without); a line that rows share is not.  s and the residual's gradient, which come back a whole block later, are stored with it:
+// joined forward 110592 x 256 bf16 37.8 us with it, 43.6 without; backward 442368 x 256 197 and 198 with inputs from memory, 169 and
+// 199 where part of them is still in the last-level cache.  y and dx are not, the next kernel reads them: joined forward 110592 x 512
+// fp16 72 us, and 90.5 together with a kernel that reads y; with the hint on y too 80.8 and 100.
 constexpr int LN_WAVES = 4;                             // of a workgroup whose teams lie within waves
 struct LnShape {
     int pieces, lanes, waves, v;                        // of a row; lanes 0: WIDE; pieces a lane has
-    int grid, past;                                     // past: what is read much later is stored past the caches
+    int grid;
     int64_t trips;                                      // rows that a team, or a workgroup, goes through
 };
 
@@ -89,11 +91,10 @@ template <int VEC, bool ODD> __device__ __forceinline__ void ln_put_sums(float *
 // Stores piece v of a row.  The overlap of an ODD row's last piece is stored twice with the same bits by one wave.  In a WIDE row the
 // two pieces may lie in different waves, and the output may lie where an input does: a wave that is ahead would overwrite what the
 // other has yet to load.  There each element is stored by the one lane that counts it, and what else that lane has loaded is not used.
-template <class T, int VEC, int V, bool ODD, bool WIDE>
+template <bool WIDE, bool PAST, class T, int VEC, int V, bool ODD>
 __device__ __forceinline__ void ln_store(typename Row<T>::elem *row, const LnLane<T, VEC, V, ODD> &at, int v,
-                                         typename Piece<T, VEC, ODD>::raw w, bool past)
+                                         typename Piece<T, VEC, ODD>::raw w)
 {
-    using P = Piece<T, VEC, ODD>;
     if constexpr (ODD && WIDE)
         if (v == V - 1 && at.skip) {
             const auto parts = __builtin_bit_cast(typename Row<T>::elems, w);
@@ -102,7 +103,7 @@ __device__ __forceinline__ void ln_store(typename Row<T>::elem *row, const LnLan
                 if (e >= at.skip) row[at.c0[v] + e] = parts.v[e];
             return;
         }
-    P::store(row + at.c0[v], w, past);
+    Piece<T, VEC, ODD>::template store<PAST>(row + at.c0[v], w);
 }
 
 // Sums over a row: its team's lanes (FULL: all 64), or the workgroup's waves through red (two arrays used in turn: between two
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_ker
         if constexpr (JOINED)                           // behind the sum, which has waited for all of the row: s may lie where x does
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (at.on[v]) ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.s) + base, at, v, out[v], q.past);
+                if (at.on[v]) ln_store<WIDE, true>(static_cast<elem *>(p.s) + base, at, v, out[v]);
         const float mean = sum[0] * inv;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_ker
         for (int v = 0; v < V; ++v) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) f[v][e] = fmaf(f[v][e] * rstd, gamma[v][e], beta[v][e]);
-            if (at.on[v]) ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.y) + base, at, v, P::pack(f[v]), false);
+            if (at.on[v]) ln_store<WIDE, false>(static_cast<elem *>(p.y) + base, at, v, P::pack(f[v]));
         }
         if (l == 0) {
             if (p.mean) p.mean[it.row] = mean;
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_ker
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) d[e] += r[e];
                 }
-                if (p.dres) ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.dres) + base, at, v, P::pack(d), q.past);
+                if (p.dres) ln_store<WIDE, true>(static_cast<elem *>(p.dres) + base, at, v, P::pack(d));
                 if (!p.dx) continue;
                 if (p.drop.t) {
                     uint32_t w[(VEC + 1) / 2];
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_ker
                     for (int e = 0; e < VEC; ++e) d[e] *= p.drop.scale;
                 }
             }
-            ln_store<T, VEC, V, ODD, WIDE>(static_cast<elem *>(p.dx) + base, at, v, P::pack(d), false);
+            ln_store<WIDE, false>(static_cast<elem *>(p.dx) + base, at, v, P::pack(d));
         }
     };
     for (int64_t k = 0; k < q.trips; k += DEPTH) {
@@ -543,7 +544,6 @@ template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd)
     q.waves = LN_WAVES;
     q.v = 1;
     q.pieces = C < E ? C : (C + E - 1) / E;
-    q.past = C >= E && n * C * (16 / E) >= 16 << 20;
     int64_t most;                                       // workgroups
     if (q.pieces <= 192) {
         if (q.pieces <= 8) q.lanes = pow2_from(q.pieces);

@@ -146,10 +146,10 @@ template <class T, int VEC, bool ANY> struct Piece {
         if constexpr (ANY) return *reinterpret_cast<const u32x4_any_t *>(p);
         else return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
     }
-    static __device__ __forceinline__ void store(elem *p, raw v, bool past = false)
+    template <bool PAST> static __device__ __forceinline__ void store(elem *p, raw v)      // PAST: past the caches
     {
         if constexpr (ANY) *reinterpret_cast<u32x4_any_t *>(p) = v;
-        else if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t *>(p));
+        else if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t *>(p));
         else *reinterpret_cast<u32x4_t *>(p) = v;
     }
     static __device__ __forceinline__ void unpack(raw w, float (&v)[VEC]) { Row<T>::unpack(w, v); }
@@ -159,7 +159,7 @@ template <class T, bool ANY> struct Piece<T, 1, ANY> {
     using elem = typename Row<T>::elem;
     using raw = elem;
     static __device__ __forceinline__ raw load(const elem *p) { return *p; }
-    static __device__ __forceinline__ void store(elem *p, raw v, bool = false) { *p = v; }
+    template <bool PAST> static __device__ __forceinline__ void store(elem *p, raw v) { *p = v; }
     static __device__ __forceinline__ void unpack(raw w, float (&v)[1]) { v[0] = Row<T>::get(w); }
     static __device__ __forceinline__ raw pack(const float (&v)[1]) { return Row<T>::put(v[0]); }
 };
