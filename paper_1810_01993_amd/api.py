@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_HERE, "libdlconv.so")
 
 DL_F16, DL_BF16, DL_F32 = 0, 1, 2
 PASS_FWD, PASS_BWD_DATA, PASS_BWD_FILTER = 0, 1, 2
+DL_ERR_SHAPE = 2
+DL_NORM_MAX_CHANNELS = 1048576
 
 EXPORTS = ("dl_conv_out_shape", "dl_conv_workspace_bytes", "dl_conv_least_workspace_bytes", "dl_conv_describe", "conv2d_fwd", "conv2d_fwd_bias_relu", "conv2d_fwd_bias_add_relu", "conv2d_bwd_data",
            "conv2d_bwd_filter", "conv2d_transpose_fwd", "conv2d_transpose_bwd_data", "conv2d_transpose_bwd_filter",
@@ -509,9 +511,12 @@ def dropout_bwd(dy: torch.Tensor, dropout: DropoutDesc, dx: torch.Tensor | None 
 
 
 def _rows(x: torch.Tensor, shape):
-    """(pixels, channels) of a [..., C] tensor."""
+    """(pixels, channels) of a [..., C] tensor.  The channels are held to the C boundary's limit here: a count beyond 32 bits would
+    arrive there modulo 2^32."""
     if not shape or shape[-1] < 1:
         raise ValueError("[..., C] tensor with C >= 1 required")
+    if shape[-1] > DL_NORM_MAX_CHANNELS:
+        raise DlError(DL_ERR_SHAPE, f"{shape[-1]} channels")
     return x.numel() // shape[-1], shape[-1]
 
 
@@ -548,6 +553,8 @@ def layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tens
 
 
 def dl_layer_norm_bwd_workspace_bytes(n_pixels: int, C: int) -> int:
+    if not (0 <= n_pixels < 1 << 63 and 1 <= C <= DL_NORM_MAX_CHANNELS):       # more would arrive modulo 2^64 and 2^32
+        raise DlError(DL_ERR_SHAPE, "dl_layer_norm_bwd_workspace_bytes")
     need = ctypes.c_size_t(0)
     _check(_lib.dl_layer_norm_bwd_workspace_bytes(n_pixels, C, ctypes.byref(need)), "dl_layer_norm_bwd_workspace_bytes")
     return need.value
