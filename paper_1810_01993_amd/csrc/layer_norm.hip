@@ -6,8 +6,8 @@
 //              dgamma = sum_pixels dy h;  dbeta = sum_pixels dy
 // The norm is that of s as stored (rounded), so that the backward pass, which has nothing else, sees the same numbers.
 //
-// Bound by memory: every tensor crosses it once.  A row stays in registers from its loads to its result, so that the variance can
-// be summed from the deviations themselves (one pass over memory, no cancellation), and the sums of the backward pass's two
+// Bound by memory: every tensor crosses it once.  A row stays in registers from its loads to its result, so that the mean can be
+// corrected and the variance summed from the deviations themselves (one pass over memory; see ln_delta), and the sums of the backward pass's two
 // parameter gradients stay in registers too.  Measured, with the bandwidth of what has to cross (a large copy reaches 5.5-5.7 TB/s):
 //   forward   1769472 x 256 fp16 316 us (5.7 TB/s), 6912 x 1024 bf16 8.1 us (3.5)
 //   backward  110592 x 304 fp16 39 us (5.1), 6912 x 2048 fp32 34 us (5.0), 208297 x 77 bf16 29 us (3.4: rows at odd addresses)
@@ -106,6 +106,22 @@ __device__ __forceinline__ void ln_store(typename Row<T>::elem *row, const LnLan
     Piece<T, VEC, ODD>::template store<PAST>(row + at.c0[v], w);
 }
 
+// The second look at a row's mean.  The first, sum * inv, is off by the roundings of the sum and of inv = 1 / C, which a mean far above
+// the spread would leave in every deviation from it (240 values of 10000: 1e-3, and y off by 0.3 gamma).  sd and sq are the sums of the
+// deviations d from the first mean and of their squares: delta = sd / C is what the first mean lacks, to the roundings of sums of d,
+// and sum (d - delta)^2 = sq - sd delta.  Rows of equal values come out exact: each d is the same few steps of the value, and the
+// quotient is rounded once (its remainder is added) and so exact too.  Where the row holds an infinity or NaN sd has no finite value and
+// the first mean stays.
+__device__ __forceinline__ float ln_delta(float &sd, float &sq, float inv, float C)
+{
+    sd = fabsf(sd) < __builtin_inff() ? sd : 0.f;
+    float delta = sd * inv;
+    delta = fmaf(fmaf(-delta, C, sd), inv, delta);
+    sq = fmaf(-sd, delta, sq);
+    sq = sq < 0.f ? 0.f : sq;                           // (NaN stays)
+    return delta;
+}
+
 // Sums over a row: its team's lanes (FULL: all 64), or the workgroup's waves through red (two arrays used in turn: between two
 // uses of one lies the other's barrier).
 template <bool FULL, bool WIDE, int N> __device__ __forceinline__ void row_sums(float (&v)[N], int lanes, float *red)
@@ -146,7 +162,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_ker
     using elem = typename P::elem;
     using raw = typename P::raw;
     constexpr int DEPTH = 2;
-    __shared__ float red[2][16];
+    __shared__ float red[3][16];
     const int lanes = WIDE ? (int)blockDim.x : FULL ? 64 : q.lanes;
     const int l = threadIdx.x & (lanes - 1);
     const LnLane<T, VEC, V, ODD> at(l, lanes, q.pieces, p.C);
@@ -173,7 +189,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_ker
     const float inv = 1.f / (float)p.C;
     auto row = [&](const Buf &b) {
         const int64_t base = it.row * p.C;
-        float f[V][VEC], sum[1] = {0.f}, sq[1] = {0.f};
+        float f[V][VEC], sum[1] = {0.f}, dev[2] = {0.f, 0.f};
         raw out[JOINED ? V : 1];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -200,24 +216,26 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_ker
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 if (at.on[v]) ln_store<WIDE, true>(static_cast<elem *>(p.s) + base, at, v, out[v]);
-        const float mean = sum[0] * inv;
+        const float first = sum[0] * inv;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[v][e] -= mean;
+            for (int e = 0; e < VEC; ++e) f[v][e] -= first;
             if (at.on[v])
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const float d = !ODD || v < V - 1 || e >= at.skip ? f[v][e] : 0.f;
-                    sq[0] = fmaf(d, d, sq[0]);
+                    dev[0] += d;
+                    dev[1] = fmaf(d, d, dev[1]);
                 }
         }
-        row_sums<FULL, WIDE>(sq, lanes, red[1]);
-        const float rstd = 1.f / sqrtf(fmaf(sq[0], inv, p.eps));
+        row_sums<FULL, WIDE>(dev, lanes, red[1]);
+        const float delta = ln_delta(dev[0], dev[1], inv, (float)p.C), mean = first + delta;
+        const float rstd = 1.f / sqrtf(fmaf(dev[1], inv, p.eps));
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[v][e] = fmaf(f[v][e] * rstd, gamma[v][e], beta[v][e]);
+            for (int e = 0; e < VEC; ++e) f[v][e] = fmaf((f[v][e] - delta) * rstd, gamma[v][e], beta[v][e]);
             if (at.on[v]) ln_store<WIDE, false>(static_cast<elem *>(p.y) + base, at, v, P::pack(f[v]));
         }
         if (l == 0) {
@@ -378,7 +396,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_ker
 
 constexpr int LN_THREADS = 256;
 
-__device__ __forceinline__ float block_sum(float v, float *red)
+template <class F> __device__ __forceinline__ F block_sum(F v, F *red)
 {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
@@ -389,19 +407,20 @@ __device__ __forceinline__ float block_sum(float v, float *red)
 }
 
 // Rows too long for the registers (more than 16384 16-bit or 8192 fp32 channels): one row per workgroup, each thread the elements
-// c = thread, thread + 256, ...; the later passes over a row find it in the caches.
+// c = thread, thread + 256, ...; the later passes over a row find it in the caches.  A thread adds up to 4096 elements one after the
+// other: the forward pass's sums are in 64 bits, in which equal values (24 bits, 2^20 of them at most) add up exactly.
 template <class T, bool JOINED>
 __global__ __launch_bounds__(LN_THREADS) void layer_norm_long_fwd_kernel(const LayerNormArgs p)
 {
     using R = Row<T>;
     using elem = typename R::elem;
-    __shared__ float red[4];
+    __shared__ double red[4];
     const Philox rng(p.drop);
     for (int64_t row = blockIdx.x; row < p.n; row += gridDim.x) {
         const int64_t base = row * p.C;
         const elem *x = static_cast<const elem *>(p.x) + base;
         const elem *s = x;
-        float sum = 0.f;
+        double sum = 0.0;
         if constexpr (JOINED) {
             const elem *res = p.residual ? static_cast<const elem *>(p.residual) + base : nullptr;
             elem *out = static_cast<elem *>(p.s) + base;
@@ -419,20 +438,20 @@ __global__ __launch_bounds__(LN_THREADS) void layer_norm_long_fwd_kernel(const L
         } else {
             for (int c = threadIdx.x; c < p.C; c += LN_THREADS) sum += R::get(x[c]);
         }
-        const float mean = block_sum(sum, red) / (float)p.C;
-        float sq = 0.f;
+        const double mean = block_sum(sum, red) / p.C;
+        double sq = 0.0;
         for (int c = threadIdx.x; c < p.C; c += LN_THREADS) {
-            const float d = R::get(s[c]) - mean;
-            sq = fmaf(d, d, sq);
+            const double d = R::get(s[c]) - mean;
+            sq = fma(d, d, sq);
         }
-        const float rstd = 1.f / sqrtf(block_sum(sq, red) / (float)p.C + p.eps);
+        const float rstd = (float)(1.0 / sqrt(block_sum(sq, red) / p.C + p.eps));
         elem *y = static_cast<elem *>(p.y) + base;
         for (int c = threadIdx.x; c < p.C; c += LN_THREADS) {
-            const float h = (R::get(s[c]) - mean) * rstd;
+            const float h = (float)(R::get(s[c]) - mean) * rstd;
             y[c] = R::put(p.gamma ? fmaf(h, p.gamma[c], p.beta[c]) : h);
         }
         if (threadIdx.x == 0) {
-            if (p.mean) p.mean[row] = mean;
+            if (p.mean) p.mean[row] = (float)mean;
             if (p.rstd) p.rstd[row] = rstd;
         }
     }
