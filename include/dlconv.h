@@ -222,13 +222,18 @@ dl_status dropout_bwd(const void *dy, const dl_dropout *dropout, int32_t dtype, 
  * F32),
  *   m = sum_c x[c] / C;  v = sum_c (x[c] - m)^2 / C;  r = 1 / sqrt(v + eps)
  *   y[c] = (x[c] - m) * r * gamma[c] + beta[c]
- * in fp32 (values whose squared distance from the mean passes fp32's range, about
- * 1e19, give r = 0), rounded once.  gamma, beta: device float[C], or both NULL (1 and 0).
- * mean, rstd: device float[n_pixels], what the backward pass takes, or NULL (not
- * written; inference).  eps finite and >= 0 (with 0 a row of equal values has
- * no finite r, and one whose variance lies below 1e-38 no finite gradient):
- * DL_ERR_VALUE otherwise.  1 <= C <= DL_NORM_MAX_CHANNELS,
- * n_pixels * C < 2^46.  y may be x.  float arrays need 4-byte alignment. */
+ * in fp32, rounded once.  The mean is corrected from the deviations: a row of equal
+ * values gives that value as m and beta as y, and a mean far above the spread costs
+ * only the rounding of m as stored.  gamma, beta: device float[C], or both NULL (1
+ * and 0).  mean, rstd: device float[n_pixels], what the backward pass takes, or NULL
+ * (not written; inference).  eps finite and >= 0, DL_ERR_VALUE otherwise; with 0 a
+ * row of equal values has no finite r.  Rows of up to 16384 16-bit or 8192 F32
+ * channels are summed in fp32: the sum of a row has to lie within its range (about
+ * 3e38; y is NaN otherwise), a sum of squared deviations beyond it (deviations of
+ * about 1.8e19 / sqrt(C)) gives r = 0, and one below 1e-38 loses digits, all of them
+ * below 1e-45 (then r is 1 / sqrt(eps)).  Longer rows are summed in 64 bits.
+ * 1 <= C <= DL_NORM_MAX_CHANNELS, n_pixels * C < 2^46.  y may be x.  float arrays
+ * need 4-byte alignment. */
 #define DL_NORM_MAX_CHANNELS 1048576
 dl_status layer_norm_fwd(const void *x, const float *gamma, const float *beta, int32_t dtype, int64_t n_pixels,
                          int32_t C, float eps, void *y, float *mean, float *rstd, void *hip_stream);
@@ -236,6 +241,7 @@ dl_status layer_norm_fwd(const void *x, const float *gamma, const float *beta, i
 /* Gradients of layer_norm_fwd, with h = (x - m) r and g = dy * gamma:
  *   dx = r * (g - sum_c g / C - h * sum_c (g * h) / C)
  *   dgamma[c] = sum over pixels of dy * h;   dbeta[c] = sum over pixels of dy
+ * in fp32, h before its products: r enters each term once, as it does the result.
  * mean, rstd: as layer_norm_fwd left them for this x.  dgamma, dbeta: device
  * float[C] (fp32 sums in a fixed order), or both NULL where gamma and beta are
  * not trained (then no workspace is needed and x and dy are still read once).

@@ -253,9 +253,10 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_fwd_ker
     }
 }
 
-// The backward pass.  With e = dy r, g = e gamma, d = s - m the row's gradient is g - sum(g) / C - d r^2 sum(g d) / C: dgamma adds
-// up e d.  The lanes that hold a channel add up its part of dgamma and dbeta over their rows in registers; at the end the teams of
-// a wave, then the waves of the workgroup are added (fixed order) and the workgroup's sums written as one slab.
+// The backward pass.  h is formed first: it lies within sqrt(C) whatever the row's spread, so that no product leaves fp32's range that
+// the gradient itself does not leave (r^2 would).  The lanes that hold a channel add up its part of dgamma and dbeta over their rows
+// in registers; at the end the teams of a wave, then the waves of the workgroup are added (fixed order) and the workgroup's sums
+// written as one slab.
 template <class T, int VEC, int V, int MODE, bool ODD, bool WIDE, bool FULL>
 __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_kernel(const LayerNormArgs p, const LnShape q)
 {
@@ -307,9 +308,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_ker
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const bool mine = !ODD || v < V - 1 || e >= at.skip;
-                h[v][e] -= mean;
+                h[v][e] = (h[v][e] - mean) * rstd;
                 db[v][e] += mine ? g[v][e] : 0.f;
-                g[v][e] *= rstd;
                 dg[v][e] = fmaf(mine ? g[v][e] : 0.f, h[v][e], dg[v][e]);
                 g[v][e] *= gamma[v][e];
                 sum[0] += mine ? g[v][e] : 0.f;
@@ -318,20 +318,18 @@ __global__ __launch_bounds__(WIDE ? 512 : 64 * LN_WAVES) void layer_norm_bwd_ker
         }
         row_sums<FULL, WIDE>(sum, lanes, red);
         if constexpr (WIDE) red = lds + (red == lds ? 32 : 0);
-        const float m0 = sum[0] * inv, m1 = sum[1] * inv * rstd * rstd;
+        const float m0 = sum[0] * inv, m1 = sum[1] * inv;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!at.on[v]) continue;
             float d[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) d[e] = fmaf(-h[v][e], m1, g[v][e] - m0);
-            if constexpr (JOINED) {
-                if constexpr (RES) {
-                    float r[VEC];
-                    P::unpack(b.ds[v], r);
+            float r[VEC];
+            if constexpr (RES) P::unpack(b.ds[v], r);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) d[e] += r[e];
-                }
+            for (int e = 0; e < VEC; ++e) d[e] = RES ? fmaf(d[e], rstd, r[e]) : d[e] * rstd;
+            if constexpr (JOINED) {
                 if (p.dres) ln_store<WIDE, true>(static_cast<elem *>(p.dres) + base, at, v, P::pack(d));
                 if (!p.dx) continue;
                 if (p.drop.t) {
