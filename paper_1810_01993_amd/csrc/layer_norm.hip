@@ -552,7 +552,8 @@ static int pow2_from(int v) { int p = 1; while (p < v) p <<= 1; return p; }
 // Up to 2048 pieces of a row stay in the registers of 8 waves.
 template <class T> static bool ln_long(int C) { return C > 2048 * Row<T>::E; }
 
-template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd)
+// params: a backward call that is asked for dgamma and dbeta.
+template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd, bool params)
 {
     constexpr int E = Row<T>::E;
     // The figures are bf16 rows, 64 M elements where no other size is given; forward first.
@@ -596,9 +597,11 @@ template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd)
         most = (bwd && q.v == 1 && n >= 16384 ? 12 : 8) * CUS / q.waves;
     }
     const int64_t per = q.lanes ? 64 * LN_WAVES / q.lanes : 1, want = (n + per - 1) / per;
-    // One workgroup's sums are the result: a few rows go through it in up to four turns, without the second launch (64 x 256 fp16
-    // 7.2 us, 10.2 with four workgroups; eight turns with dropout take longer than that launch).
-    if (bwd && want <= 4) most = 1;
+    // One workgroup's sums are the result: where dgamma and dbeta are asked for, a few rows go through it in turns, without the second
+    // launch.  (Each call behind another in a graph.)  Four turns of teams: 64 x 256 fp16 5.9 us, 6.3 with four workgroups, joined 7.8
+    // and 6.9; two turns 4.9 and 6.6 (8 x 1024), joined 6.0 and 7.3.  Two rows that a workgroup has to itself: 2 x 2048 3.5 and 5.1, 2 x
+    // 16384 8.6 and 11.8, joined 12.6 and 14.5; with four of them it does not pay (4 x 16384 13.0 and 12.0, joined 20.8 and 14.7).
+    if (params && want <= (q.lanes ? 4 : 2)) most = 1;
     q.grid = (int)std::max<int64_t>(1, std::min(want, most));
     q.trips = (want + q.grid - 1) / q.grid;
     return q;
@@ -608,8 +611,8 @@ static int ln_long_slabs(int64_t n) { return (int)std::max<int64_t>(1, std::min<
 
 int layer_norm_slabs(int64_t n, int C)
 {
-    const int half = ln_long<F16>(C) ? ln_long_slabs(n) : ln_shape<F16>(n, C, true).grid;
-    const int whole = ln_long<F32>(C) ? ln_long_slabs(n) : ln_shape<F32>(n, C, true).grid;
+    const int half = ln_long<F16>(C) ? ln_long_slabs(n) : ln_shape<F16>(n, C, true, true).grid;
+    const int whole = ln_long<F32>(C) ? ln_long_slabs(n) : ln_shape<F32>(n, C, true, true).grid;
     return std::max(half, whole);
 }
 
@@ -656,7 +659,7 @@ static hipError_t ln_resident(const LayerNormArgs &a, const LnShape &q, bool bwd
 template <class T>
 static hipError_t launch_ln_fwd(const LayerNormArgs &a, hipStream_t stream)
 {
-    if (!ln_long<T>(a.C)) return ln_resident<T>(a, ln_shape<T>(a.n, a.C, false), false, stream);
+    if (!ln_long<T>(a.C)) return ln_resident<T>(a, ln_shape<T>(a.n, a.C, false, false), false, stream);
     const dim3 grid((unsigned)std::min<int64_t>(a.n, 1 << 20)), block(LN_THREADS);
     if (a.joined) DLK_LAUNCH("layer_norm_long_fwd_kernel", (layer_norm_long_fwd_kernel<T, true>), grid, block, 0, stream, a);
     else DLK_LAUNCH("layer_norm_long_fwd_kernel", (layer_norm_long_fwd_kernel<T, false>), grid, block, 0, stream, a);
@@ -685,7 +688,7 @@ static hipError_t launch_ln_bwd(const LayerNormArgs &a0, hipStream_t stream)
     const dim3 block(LN_THREADS);
     hipError_t e;
     if (a.n > 0 && !ln_long<T>(a.C)) {
-        const LnShape q = ln_shape<T>(a.n, a.C, true);
+        const LnShape q = ln_shape<T>(a.n, a.C, true, a.dgamma);
         e = ln_resident<T>(a, q, true, stream);
         return e != hipSuccess || !a.dgamma || q.grid == 1 ? e : ln_param_sum(a, q.grid, stream);
     }
