@@ -9,11 +9,13 @@
 // Bound by memory: every tensor crosses it once.  A row stays in registers from its loads to its result, so that the mean can be
 // corrected and the variance summed from the deviations themselves (one pass over memory; see ln_delta), and the sums of the backward pass's two
 // parameter gradients stay in registers too.  Measured, with the bandwidth of what has to cross (a large copy reaches 5.5-5.7 TB/s):
-//   forward   1769472 x 256 fp16 316 us (5.7 TB/s), 6912 x 1024 bf16 8.1 us (3.5)
-//   backward  110592 x 304 fp16 39 us (5.1), 6912 x 2048 fp32 34 us (5.0), 208297 x 77 bf16 29 us (3.4: rows at odd addresses)
-//   joined    forward 110592 x 256 bf16 38 us (6.0), backward 442368 x 256 bf16 197 us (5.8), 3015 x 512 fp16 10.5 us (1.5: two
-//             launches, 8 and 3 us on their own)
-// Of a backward call about 4.7 us are the second launch, which adds the workgroups' sums in a fixed order.
+//   forward   1769472 x 256 fp16 319 us (5.7 TB/s), 6912 x 1024 bf16 8.2 us (3.4)
+//   backward  110592 x 304 fp16 40 us (5.1), 6912 x 2048 fp32 35 us (4.9), 208297 x 77 bf16 29 us (3.4: too little in flight, see
+//             ln_shape)
+//   joined    forward 110592 x 256 bf16 38 us (6.0), backward 442368 x 256 bf16 196 us (5.8), 3015 x 512 fp16 10.9 us (1.4: two
+//             launches, 8.0 and 2.6 us on their own)
+// The second launch of a backward call, which adds the workgroups' sums in a fixed order, shows 2.6 to 4.9 us in these cases; calls
+// without parameter gradients and those that one workgroup does alone have none.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,7 +30,8 @@ namespace dlk {
 // rows), or, WIDE, a whole workgroup has one.  Lane l owns the 16-byte pieces l, l + lanes, ... (V at most) of its row: it reads
 // them once, keeps them in registers through both sums and the result, and has the next row's pieces on their way meanwhile.
 // Rows that are no whole number of pieces (ODD) end in a piece that reaches back over what the one before it covers: the elements
-// that both hold are counted once and stored twice, with the same bits.  VEC = 1: rows shorter than a piece.
+// that both hold are counted once and, in a team's row, stored twice, with the same bits (in a WIDE one once, see ln_store).  VEC = 1:
+// rows shorter than a piece.
 //
 // Whole pieces are loaded with the hint that nobody reads the line again (backward 110592 x 256 fp16: 35.1 us with it, 38.1
 // without); a line that rows share is not.  s and the residual's gradient, which come back a whole block later, are stored with it:
@@ -406,7 +409,9 @@ template <class F> __device__ __forceinline__ F block_sum(F v, F *red)
 
 // Rows too long for the registers (more than 16384 16-bit or 8192 fp32 channels): one row per workgroup, each thread the elements
 // c = thread, thread + 256, ...; the later passes over a row find it in the caches.  A thread adds up to 4096 elements one after the
-// other: the forward pass's sums are in 64 bits, in which equal values (24 bits, 2^20 of them at most) add up exactly.
+// other: the forward pass's sums are in 64 bits, in which equal values (24 bits, 2^20 of them at most) add up exactly.  Simple, and far from memory's
+// rate: an element a load, several passes, a block of random numbers an element.  4096 x 16392 fp16 forward 203 us (1.3 TB/s; 197 with
+// sums in 32 bits), backward 239 us (1.7), joined 400 and 451 us.
 template <class T, bool JOINED>
 __global__ __launch_bounds__(LN_THREADS) void layer_norm_long_fwd_kernel(const LayerNormArgs p)
 {
@@ -549,7 +554,9 @@ __global__ __launch_bounds__(1024) void layer_norm_param_sum_kernel(const float 
 constexpr int CUS = 256;
 static int pow2_from(int v) { int p = 1; while (p < v) p <<= 1; return p; }
 
-// Up to 2048 pieces of a row stay in the registers of 8 waves.
+// Up to 2048 pieces of a row stay in the registers of 8 waves.  (The joined backward pass with ds at four pieces a lane, 12289 to 16384
+// 16-bit channels, needs a few more than the 256 there are: 9 to 17 words a lane go through scratch memory.  2000 x 16384 fp16 87 us,
+// 3.8 TB/s.)
 template <class T> static bool ln_long(int C) { return C > 2048 * Row<T>::E; }
 
 // params: a backward call that is asked for dgamma and dbeta.
@@ -584,8 +591,9 @@ template <class T> static LnShape ln_shape(int64_t n, int C, bool bwd, bool para
         // Loads under way, not more: from 64 MB on 8 waves a compute unit with two or three pieces a lane, 16 with one (1769472 x 256
         // fp16 318 us with 8 waves, 367 with 16: fewer rows at a time stay within fewer memory pages); twice that on smaller tensors,
         // where a wave has few rows (8192 x 1024 9.0 us, 9.4 with half).  Backward, where each workgroup's sums are a slab of the
-        // workspace, half as many: 256 slabs with two pieces or more (65536 x 1024 67.9 us, 70.6 with 512), 768 with one (96 channels
-        // 71.9, with 256 116).
+        // workspace, 4 waves (256 slabs) with two pieces or more (65536 x 1024 67.9 us, 70.6 with 512), 12 (768) with one (96 channels
+        // 71.9, with 256 116).  Rows that leave many lanes idle have little under way all the same: at 77 channels 10 of 16 lanes hold a
+        // piece, 15 KB a compute unit for a row of dy and x each (304 channels: 19 KB, and 5.1 TB/s for 3.4).
         most = bwd ? (q.v == 1 ? 3 : 1) * CUS : (q.v == 1 ? 8 : 4) * CUS / (large ? 2 : 1);
     } else {
         // As few waves a row as its registers allow, since they wait for each other at two barriers (one, backward): up to four
