@@ -7,8 +7,9 @@
 // The norm is that of s as stored (rounded), so that the backward pass, which has nothing else, sees the same numbers.
 //
 // Bound by memory: every tensor crosses it once.  A row stays in registers from its loads to its result, so that the mean can be
-// corrected and the variance summed from the deviations themselves (one pass over memory; see ln_delta), and the sums of the backward pass's two
-// parameter gradients stay in registers too.  Measured, with the bandwidth of what has to cross (a large copy reaches 5.5-5.7 TB/s):
+// corrected and the variance summed from the deviations themselves (one pass over memory; see ln_delta), and the sums of the backward
+// pass's two parameter gradients stay in registers too.  Measured, with the bandwidth of what has to cross (a large copy reaches
+// 5.5-5.7 TB/s):
 //   forward   1769472 x 256 fp16 319 us (5.7 TB/s), 6912 x 1024 bf16 8.2 us (3.4)
 //   backward  110592 x 304 fp16 40 us (5.1), 6912 x 2048 fp32 35 us (4.9), 208297 x 77 bf16 29 us (3.4: too little in flight, see
 //             ln_shape)
@@ -409,9 +410,9 @@ template <class F> __device__ __forceinline__ F block_sum(F v, F *red)
 
 // Rows too long for the registers (more than 16384 16-bit or 8192 fp32 channels): one row per workgroup, each thread the elements
 // c = thread, thread + 256, ...; the later passes over a row find it in the caches.  A thread adds up to 4096 elements one after the
-// other: the forward pass's sums are in 64 bits, in which equal values (24 bits, 2^20 of them at most) add up exactly.  Simple, and far from memory's
-// rate: an element a load, several passes, a block of random numbers an element.  4096 x 16392 fp16 forward 203 us (1.3 TB/s; 197 with
-// sums in 32 bits), backward 239 us (1.7), joined 400 and 451 us.
+// other: the forward pass's sums are in 64 bits, in which equal values (24 bits, 2^20 of them at most) add up exactly.  Simple, and far
+// from memory's rate: an element a load, several passes, a block of random numbers an element.  4096 x 16392 fp16 forward 203 us
+// (1.3 TB/s; 197 with sums in 32 bits), backward 239 us (1.7), joined 400 and 451 us.
 template <class T, bool JOINED>
 __global__ __launch_bounds__(LN_THREADS) void layer_norm_long_fwd_kernel(const LayerNormArgs p)
 {
